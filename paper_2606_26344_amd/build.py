@@ -11,19 +11,20 @@ from __future__ import annotations
 import os
 import subprocess
 import sys
+from concurrent.futures import ThreadPoolExecutor
 
 PKG = os.path.dirname(os.path.abspath(__file__))
 ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIBRARY = os.path.join(PKG, "libgmlp.so")
-SOURCES = [os.path.join(CSRC, "gmlp.hip")]
+SOURCES = [os.path.join(CSRC, f) for f in ("gmlp.hip", "train.hip")]
 # A measuring program beside the library (not part of it): the board's
 # sustained bf16 matrix-core rate, which bench.py reports as context.
 MFMA_CEILING = os.path.join(PKG, "mfma_ceiling")
 MFMA_CEILING_SOURCE = os.path.join(CSRC, "mfma_ceiling.hip")
 HEADERS = [os.path.join(CSRC, f) for f in sorted(os.listdir(CSRC)) if f.endswith(".hpp")] + [
-    os.path.join(INCLUDE, h) for h in ("gmlp.h", "softmax_matmul.h")]
+    os.path.join(INCLUDE, h) for h in ("gmlp.h", "softmax_matmul.h", "gmlp_train.h")]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [
@@ -69,7 +70,18 @@ def _compile(out, flags, sources, verbose):
 def build(verbose: bool = False, extra_flags=()) -> str:
     """Compile libgmlp.so (and the mfma_ceiling program) next to this file;
     returns the library's path."""
-    _compile(LIBRARY, [*FLAGS, *extra_flags], SOURCES, verbose)
+    # One object per source, compiled side by side, then linked.
+    flags = [f for f in FLAGS if f != "-shared"]
+    objects = [LIBRARY + ".tmp%d.%d.o" % (os.getpid(), i) for i in range(len(SOURCES))]
+    try:
+        with ThreadPoolExecutor(max_workers=4) as pool:
+            list(pool.map(lambda so: _compile(so[1], [*flags, *extra_flags, "-c"], [so[0]], verbose),
+                          zip(SOURCES, objects)))
+        _compile(LIBRARY, ["--offload-arch=gfx950", "-shared", "-fPIC", *extra_flags], objects, verbose)
+    finally:
+        for o in objects:
+            if os.path.exists(o):
+                os.remove(o)
     exe_flags = [f for f in FLAGS if f not in ("-shared", "-fPIC")]
     _compile(MFMA_CEILING, exe_flags, [MFMA_CEILING_SOURCE], verbose)
     return LIBRARY

@@ -18,6 +18,7 @@ enum Epilogue {
     EPI_GATE_MUL = 0, // out = bf16(act(acc0) * acc1)    (H of the gate/up step)
     EPI_STORE = 1,    // out = bf16(acc0)                (Y of the down step)
     EPI_GATE_PAIR = 2, // out = bf16(act(G) * U), G and U from the two blocks of a pair
+    EPI_GATE_SAVE = 3, // EPI_GATE_MUL, and G and U themselves as bf16 (for a backward pass)
 };
 
 #define GMLP_LDS(p) ((__attribute__((address_space(3))) void *)(p))

@@ -734,6 +734,27 @@ __device__ __forceinline__ int gemm_block(const GemmParams &p, int block, StageP
         }
     const bool scaled = EPI == EPI_GATE_MUL && p.rrms;
     const bool divided = EPI == EPI_STORE && p.rowdiv;
+    if constexpr (EPI == EPI_GATE_SAVE) {
+        // G and U, each rounded once; H below takes the unrounded values.
+        const __amdgpu_buffer_rsrc_t rg = make_rsrc(p.out_g + (size_t)n0 * M + m0);
+        const __amdgpu_buffer_rsrc_t ru = make_rsrc(p.out_u + (size_t)n0 * M + m0);
+#pragma unroll
+        for (int mi = 0; mi < TM; ++mi)
+#pragma unroll
+            for (int ni = 0; ni < TN; ++ni)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int fl = wm * TM * 32 + mi * 32 + A::col(j, lane);
+                    const int tl = wn * TN * 32 + ni * 32 + A::tok(j, lane);
+                    const uint32_t off = n0 + tl < N && m0 + fl < M ? (uint32_t)(tl * M + fl) * 2u : kOutOfRange;
+                    const f32x4 g = acc[0][mi][ni].piece(j), u = acc[NW - 1][mi][ni].piece(j);
+                    __builtin_amdgcn_raw_buffer_store_b64(u32x2{pack_bf16x2(g[0], g[1]), pack_bf16x2(g[2], g[3])}, rg,
+                                                          off, 0, OUT_POLICY);
+                    __builtin_amdgcn_raw_buffer_store_b64(u32x2{pack_bf16x2(u[0], u[1]), pack_bf16x2(u[2], u[3])}, ru,
+                                                          off, 0, OUT_POLICY);
+                    __builtin_amdgcn_sched_barrier(0);
+                }
+    }
     // All of the wave's packed results first, each group of 4 columns into
     // registers of its own, then the stores back to back: a store's data
     // registers are not overwritten while it is in flight, so no store waits
@@ -749,7 +770,7 @@ __device__ __forceinline__ int gemm_block(const GemmParams &p, int block, StageP
                 float v[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    if constexpr (EPI == EPI_GATE_MUL) {
+                    if constexpr (EPI == EPI_GATE_MUL || EPI == EPI_GATE_SAVE) {
                         float g = acc[0][mi][ni].get(4 * j + e), u = acc[NW - 1][mi][ni].get(4 * j + e);
                         if (scaled) {
                             g *= rs[ni][h];

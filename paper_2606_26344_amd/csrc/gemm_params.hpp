@@ -34,6 +34,8 @@ struct GemmParams {
     // Store epilogue: per-token divisors [N] (nullptr: none).  Softmax+MatMul
     // divides its result rows by the softmax sums here.
     const float *rowdiv;
+    // EPI_GATE_SAVE: G and U as bf16, [N, M], beside H.
+    uint16_t *out_g, *out_u;
 };
 
 } // namespace gmlp

@@ -3,8 +3,7 @@
 // static analogue of the paper's empirical per-shape selection, Section
 // 4.6), and the workspace layout.  Plain C++ with no HIP dependency, so that
 // it can also be built and exercised on the host alone (the sanitizer test
-// builds it with AddressSanitizer and UndefinedBehaviorSanitizer).  Included
-// by one translation unit per program.
+// builds it with AddressSanitizer and UndefinedBehaviorSanitizer).
 #pragma once
 
 #include <algorithm>
@@ -21,11 +20,14 @@
 #include "tiling.hpp"
 
 namespace gmlp {
+
+// The last error of the calling thread (gmlp_last_error), one for all
+// translation units of the library.
+inline thread_local char g_err[512];
+
 namespace {
 
-thread_local char g_err[512];
-
-int fail(int code, const char *fmt, ...)
+inline int fail(int code, const char *fmt, ...)
 {
     va_list ap;
     va_start(ap, fmt);
@@ -34,7 +36,7 @@ int fail(int code, const char *fmt, ...)
     return code;
 }
 
-int ok()
+inline int ok()
 {
     g_err[0] = '\0';
     return GMLP_OK;
@@ -114,7 +116,7 @@ constexpr int64_t kMaxElements = int64_t(1) << 37;
 // Whether any of the [rows, a], [rows, b] and [a, b] tensors of a shape has
 // more than kMaxElements elements (each factor already within its limit, so
 // the products fit in int64).
-bool too_many_elements(int64_t rows, int64_t a, int64_t b)
+inline bool too_many_elements(int64_t rows, int64_t a, int64_t b)
 {
     return rows * a > kMaxElements || rows * b > kMaxElements || a * b > kMaxElements;
 }
@@ -132,8 +134,8 @@ constexpr size_t kReadyBytes = (size_t)kFusedMaxSplits * kFlagStride * sizeof(ui
 constexpr size_t kErrorOffset = kStripCounterBytes + kReadyBytes;
 constexpr size_t kCounterBytes = kErrorOffset + 256;
 
-size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
-int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
+inline size_t align_up(size_t x) { return (x + kAlign - 1) / kAlign * kAlign; }
+inline int64_t cdiv(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 enum Kind {
     K_NONE,
@@ -170,7 +172,7 @@ struct Step {
 
 // The split part of a step with a tail: its last tail_tiles tiles, split
 // over K (launched after the step's tile_count whole-tile blocks).
-Step tail_step(const Step &s)
+inline Step tail_step(const Step &s)
 {
     Step t = s;
     t.tile_base = s.tile_count;
@@ -194,7 +196,7 @@ struct Plan {
 
 // Arrival counters the steps of a two-kernel plan use, from the start of the
 // counter block.
-int plan_counters(const Plan &p)
+inline int plan_counters(const Plan &p)
 {
     return std::max({p.gate_up.counters, p.gate_up_rest.counters, p.down.counters});
 }
@@ -227,7 +229,7 @@ constexpr int kWideDownBelowRows = 64 * DownLarge::BK;
 // keeping at least `min_tiles` k-tiles of `tile_k` rows per split.  Each
 // split adds T x columns fp32 partial sums to write and read back, so the
 // count rounds down.
-void choose_splits(Step &s, int tiles, int target, int tile_k, int min_tiles)
+inline void choose_splits(Step &s, int tiles, int target, int tile_k, int min_tiles)
 {
     const int64_t ktiles = cdiv(s.K, tile_k);
     int64_t splits = 1;
@@ -243,7 +245,7 @@ void choose_splits(Step &s, int tiles, int target, int tile_k, int min_tiles)
 // the ring kernels reach: 0.66 us for the 128 x 128 down tiles, 0.98 for the
 // gate/up ones), an exchange 4 us, the partial tile of each split read by the
 // last block at 54 GB/s, and all blocks' partial tiles written at 8 TB/s.
-double split_time(int64_t ktiles, int64_t splits, int64_t tiles, size_t stage_bytes, size_t tile_bytes)
+inline double split_time(int64_t ktiles, int64_t splits, int64_t tiles, size_t stage_bytes, size_t tile_bytes)
 {
     const double t = (double)ktiles * (double)stage_bytes / 50e3;
     if (splits == 1)
@@ -260,7 +262,7 @@ double split_time(int64_t ktiles, int64_t splits, int64_t tiles, size_t stage_by
 // count stays (T = 222, D = 4096, F = 16384: 4 splits of the down step).  The
 // 256-column down tiles, which are chosen by the length of their splits, keep
 // the other rule.
-void choose_splits_by_time(Step &s, int tiles, int target, int tile_k, size_t stage_bytes, size_t tile_bytes)
+inline void choose_splits_by_time(Step &s, int tiles, int target, int tile_k, size_t stage_bytes, size_t tile_bytes)
 {
     const int64_t ktiles = cdiv(s.K, tile_k);
     const int64_t most = tiles < target ? std::min<int64_t>(target / tiles, std::max<int64_t>(1, ktiles / 2)) : 1;
@@ -409,7 +411,7 @@ constexpr int kStreamWideTokens = 16; // the 128-column tiles: one 16-token tile
 //     several rounds, and up to 80 tokens the streaming tiles win again (D = 49152,
 //     K = 320: T = 64 19.3 -> 14.3, 90 20.1 -> 20.9; T = 120, D = 33000, K = 504 24.6 ->
 //     29.9).
-bool stream_slower(int64_t n, int64_t M, int64_t K, bool gate_up)
+inline bool stream_slower(int64_t n, int64_t M, int64_t K, bool gate_up)
 {
     if (gate_up && n > 80 && K <= (n > 96 ? 192 : 64))
         return true;
@@ -452,7 +454,7 @@ bool stream_slower(int64_t n, int64_t M, int64_t K, bool gate_up)
 // gate/up 21.1 -> 18.2, 25.9 -> 23.4, D = 4096, F = 11008 37.1 -> 36.5 (kept).
 // Gate/up steps of more than 96 128-column tiles keep the ring (pairs above
 // 64 tokens): they fill the chip without splits shorter than half of K.
-int stream_width(int64_t n, int64_t M, int64_t K, bool gate_up)
+inline int stream_width(int64_t n, int64_t M, int64_t K, bool gate_up)
 {
     if (n > kStreamMaxTokens || (gate_up && cdiv(M, 128) >= (kPairMinBlocks + 1) / 2))
         return 0;
@@ -497,7 +499,7 @@ auto with_stream_tile(const Step &s, F f)
 //     14.7 (20.5); T = 120, K = 1288, F = 4096 24.2, 21.6 (29.1); T = 128, K = 1160,
 //     F = 4096 21.4, 22.3.
 //   Longer K: T = 69, K = 6888, F = 544 11 splits of 640 rows 20.7, 27 of 256 25.0.
-int stream_min_k_tiles(int wm, int M, int N, int K, bool gate_up)
+inline int stream_min_k_tiles(int wm, int M, int N, int K, bool gate_up)
 {
     if (wm == 4)
         return 2;
@@ -514,7 +516,7 @@ int stream_min_k_tiles(int wm, int M, int N, int K, bool gate_up)
     }
 }
 
-void stream_step(Step &s, int wm, int M, int N, int K, bool gate_up)
+inline void stream_step(Step &s, int wm, int M, int N, int K, bool gate_up)
 {
     s.stream_wm = wm;
     s.N = N;
@@ -530,7 +532,7 @@ void stream_step(Step &s, int wm, int M, int N, int K, bool gate_up)
 
 // Rows per load batch of all row groups of a block, per token count and
 // step (splits are whole batches).
-int gemv_batch_span(int nt, int nw)
+inline int gemv_batch_span(int nt, int nw)
 {
     const int rg = gemv_threads(nt) / gemv_strip_lanes(nt, nw);
     auto rows = [nw](auto ntc) {
@@ -561,9 +563,9 @@ int gemv_batch_span(int nt, int nw)
 // take the registers), so two 4-wave blocks per CU keep enough loads in
 // flight (measured: T = 5, 6 are 9% and 4% faster with one block per CU,
 // T = 7, 8 6% and 11% slower).
-int gemv_block_target(int nt) { return nt <= 6 ? 256 : 512; }
+inline int gemv_block_target(int nt) { return nt <= 6 ? 256 : 512; }
 
-void gemv_step(Step &s, int M, int N, int K, int nw)
+inline void gemv_step(Step &s, int M, int N, int K, int nw)
 {
     s.kind = K_GEMV;
     s.M = M;
@@ -589,7 +591,7 @@ void gemv_step(Step &s, int M, int N, int K, int nw)
     s.partial_bytes = s.splits > 1 ? (size_t)s.splits * ((size_t)nw * N * M + (size_t)s.strips * N) * sizeof(float) : 0;
 }
 
-Plan make_plan(int64_t T, int64_t D, int64_t F, int path)
+inline Plan make_plan(int64_t T, int64_t D, int64_t F, int path)
 {
     Plan p;
     const int asked = path;
@@ -798,14 +800,14 @@ Plan make_plan(int64_t T, int64_t D, int64_t F, int path)
 
 // Whether both steps' split-K counters of a one-launch MFMA plan fit in the
 // counter block together (down's follow gate/up's).
-bool fused_mfma_counters_fit(const Plan &p)
+inline bool fused_mfma_counters_fit(const Plan &p)
 {
     return (size_t)(p.gate_up.tile_count + p.down.counters) * sizeof(uint32_t) <= kStripCounterBytes;
 }
 
 // One layout serves every path, so a workspace sized by gmlp_workspace_size
 // fits whichever kernels run.
-Layout make_layout(int64_t T, int64_t D, int64_t F)
+inline Layout make_layout(int64_t T, int64_t D, int64_t F)
 {
     // T = 0 launches nothing; its workspace is sized as for one token (the
     // plans below need at least one token tile).
@@ -841,15 +843,15 @@ Layout make_layout(int64_t T, int64_t D, int64_t F)
     return l;
 }
 
-bool misaligned(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) != 0; }
+inline bool misaligned(const void *p) { return (reinterpret_cast<uintptr_t>(p) & 15) != 0; }
 
-bool overlaps(const void *a, size_t an, const void *b, size_t bn)
+inline bool overlaps(const void *a, size_t an, const void *b, size_t bn)
 {
     const uintptr_t x = reinterpret_cast<uintptr_t>(a), y = reinterpret_cast<uintptr_t>(b);
     return an && bn && x < y + bn && y < x + an;
 }
 
-int check_shape(int64_t T, int64_t D, int64_t F)
+inline int check_shape(int64_t T, int64_t D, int64_t F)
 {
     if (T < 0 || D <= 0 || F <= 0)
         return fail(GMLP_ERR_INVALID_ARG, "invalid shape T=%lld D=%lld F=%lld (need T >= 0, D > 0, F > 0)",
@@ -864,7 +866,7 @@ int check_shape(int64_t T, int64_t D, int64_t F)
     return GMLP_OK;
 }
 
-int check_ptr(const void *p, const char *name, bool required)
+inline int check_ptr(const void *p, const char *name, bool required)
 {
     if (!p)
         return required ? fail(GMLP_ERR_INVALID_ARG, "%s is NULL", name) : GMLP_OK;
@@ -873,7 +875,7 @@ int check_ptr(const void *p, const char *name, bool required)
     return GMLP_OK;
 }
 
-int validate(int64_t T, int64_t D, int64_t F, const void *X, const void *Wg, const void *Wu,
+inline int validate(int64_t T, int64_t D, int64_t F, const void *X, const void *Wg, const void *Wu,
              const void *Wd, const void *Y)
 {
     int rc;
@@ -893,13 +895,13 @@ int validate(int64_t T, int64_t D, int64_t F, const void *X, const void *Wg, con
 
 // Weights are streamed (nontemporal loads) when the plan has a single token
 // tile: then each weight element is read by one block only.
-bool stream_weights(const Step &s) { return s.tiles_n == 1; }
+inline bool stream_weights(const Step &s) { return s.tiles_n == 1; }
 
 // The fused kernel: the gate/up items on the first blocks, the down items on
 // the rest, all in one launch.
-int fused_grid(const Plan &plan) { return plan.gate_up.blocks + plan.down.blocks; }
+inline int fused_grid(const Plan &plan) { return plan.gate_up.blocks + plan.down.blocks; }
 
-int check_variant(int activation, float beta, int rmsnorm, float eps, Variant *v)
+inline int check_variant(int activation, float beta, int rmsnorm, float eps, Variant *v)
 {
     if (activation != GMLP_ACT_SILU && activation != GMLP_ACT_SWISH && activation != GMLP_ACT_SIGMOID)
         return fail(GMLP_ERR_INVALID_ARG, "unknown activation %d", activation);
@@ -916,7 +918,7 @@ int check_variant(int activation, float beta, int rmsnorm, float eps, Variant *v
     return GMLP_OK;
 }
 
-int check_path(int path, int64_t T)
+inline int check_path(int path, int64_t T)
 {
     if (path != GMLP_PATH_AUTO && path != GMLP_PATH_GEMV && path != GMLP_PATH_MFMA && path != GMLP_PATH_FUSED &&
         path != GMLP_PATH_FUSED_MFMA)
@@ -932,14 +934,14 @@ int check_path(int path, int64_t T)
 
 // The entry points that run one step alone (and Softmax+MatMul) have no
 // fused form.
-int check_single_step_path(int path, int64_t T)
+inline int check_single_step_path(int path, int64_t T)
 {
     if (path == GMLP_PATH_FUSED || path == GMLP_PATH_FUSED_MFMA)
         return fail(GMLP_ERR_UNSUPPORTED, "the fused paths run the whole Gated MLP only");
     return check_path(path, T);
 }
 
-int check_workspace(void *ws, size_t ws_bytes, const Layout &l)
+inline int check_workspace(void *ws, size_t ws_bytes, const Layout &l)
 {
     if (!ws)
         return fail(GMLP_ERR_INVALID_ARG, "workspace is NULL");
@@ -962,7 +964,7 @@ std::string shape_name()
 }
 
 // A step's kernel as a profiler names it, without the namespace.
-std::string kernel_name(const Step &s, bool gate_up)
+inline std::string kernel_name(const Step &s, bool gate_up)
 {
     switch (s.kind) {
     case K_GEMM_GU_L:
@@ -1009,7 +1011,7 @@ std::string kernel_name(const Step &s, bool gate_up)
 }
 
 // The kernel of a fused plan as a profiler names it, without the namespace.
-std::string fused_kernel_name(const Plan &plan)
+inline std::string fused_kernel_name(const Plan &plan)
 {
     if (plan.path == GMLP_PATH_FUSED)
         return "gemv_fused_kernel<" + std::to_string(plan.gate_up.N) + ", false>";
@@ -1019,7 +1021,7 @@ std::string fused_kernel_name(const Plan &plan)
 }
 
 // The describe line of a step's launch.
-std::string describe_step(const Step &s, bool gate_up)
+inline std::string describe_step(const Step &s, bool gate_up)
 {
     char tmp[200];
     if (s.tail_tiles) {
@@ -1036,7 +1038,7 @@ std::string describe_step(const Step &s, bool gate_up)
     return tmp;
 }
 
-int check_gate_up_args(const void *X, const void *Wg, const void *Wu, const void *H, int64_t T,
+inline int check_gate_up_args(const void *X, const void *Wg, const void *Wu, const void *H, int64_t T,
                        int64_t D, int64_t F)
 {
     int rc;
@@ -1050,7 +1052,7 @@ int check_gate_up_args(const void *X, const void *Wg, const void *Wu, const void
     return GMLP_OK;
 }
 
-int check_down_args(const void *H, const void *Wd, const void *Y, int64_t T, int64_t F, int64_t D)
+inline int check_down_args(const void *H, const void *Wd, const void *Y, int64_t T, int64_t F, int64_t D)
 {
     int rc;
     if ((rc = check_shape(T, D, F)) || (rc = check_ptr(H, "H", T > 0)) ||
@@ -1063,7 +1065,7 @@ int check_down_args(const void *H, const void *Wd, const void *Y, int64_t T, int
 }
 
 
-int check_smm_shape(int64_t M, int64_t K, int64_t N)
+inline int check_smm_shape(int64_t M, int64_t K, int64_t N)
 {
     if (M < 0 || K <= 0 || N <= 0)
         return fail(GMLP_ERR_INVALID_ARG, "invalid shape M=%lld K=%lld N=%lld (need M >= 0, K > 0, N > 0)",
@@ -1078,7 +1080,7 @@ int check_smm_shape(int64_t M, int64_t K, int64_t N)
     return GMLP_OK;
 }
 
-int check_smm_args(const void *X, const void *Y, const void *Z, int64_t M, int64_t K, int64_t N)
+inline int check_smm_args(const void *X, const void *Y, const void *Z, int64_t M, int64_t K, int64_t N)
 {
     int rc;
     if ((rc = check_smm_shape(M, K, N)))
@@ -1095,7 +1097,7 @@ int check_smm_args(const void *X, const void *Y, const void *Z, int64_t M, int64
 // shapes of the benchmark (K = N = 8192) it beats the 32-token MFMA tiles at
 // every M <= 8 (measured: 33.0 against 34.2 us at M = 8), unlike the
 // Gated MLP's pair of steps.
-Step smm_matmul_step(int64_t M, int64_t K, int64_t N, int path)
+inline Step smm_matmul_step(int64_t M, int64_t K, int64_t N, int path)
 {
     if (path == GMLP_PATH_AUTO && M <= kGemvMaxTokens)
         path = GMLP_PATH_GEMV;
@@ -1105,7 +1107,7 @@ Step smm_matmul_step(int64_t M, int64_t K, int64_t N, int path)
 // Counter block, then P [M, K] bf16 (in the H slot), the matmul's split-K
 // partial sums, and the row sums [M] fp32 (in the row-scale slot).  Sized for
 // every path of the shape.
-Layout smm_layout(int64_t M, int64_t K, int64_t N)
+inline Layout smm_layout(int64_t M, int64_t K, int64_t N)
 {
     M = std::max<int64_t>(M, 1); // as for make_layout: M = 0 launches nothing
     int counters = 0;

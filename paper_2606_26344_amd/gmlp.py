@@ -33,7 +33,8 @@ import torch
 HERE = os.path.dirname(os.path.abspath(__file__))
 LIBRARY = os.path.join(HERE, "libgmlp.so")
 HEADER = os.path.join(os.path.dirname(HERE), "include", "gmlp.h")
-HEADERS = [HEADER, os.path.join(os.path.dirname(HERE), "include", "softmax_matmul.h")]
+HEADERS = [os.path.join(os.path.dirname(HERE), "include", h)
+           for h in ("gmlp.h", "softmax_matmul.h", "gmlp_train.h")]
 
 PATH_AUTO, PATH_GEMV, PATH_MFMA, PATH_FUSED, PATH_FUSED_MFMA = 0, 1, 2, 3, 4
 _PATHS = {"auto": PATH_AUTO, "gemv": PATH_GEMV, "mfma": PATH_MFMA, "fused": PATH_FUSED,
@@ -79,6 +80,10 @@ _SIGNATURES = {
     "softmax_matmul": ([_P, _P, _P, _I64, _I64, _I64, _P], _INT),
     "softmax_matmul_exp_rows": ([_P, _P, _P, _I64, _I64, _P], _INT),
     "softmax_matmul_divide_ws": ([_P, _P, _P, _P, _I64, _I64, _I64, _INT, _P, _SZ, _P], _INT),
+    "gmlp_train_workspace_size": ([_I64, _I64, _I64], _SZ),
+    "gmlp_train_describe": ([_I64, _I64, _I64, _INT, ctypes.c_char_p, _SZ], _INT),
+    "gmlp_train_forward": ([_P] * 7 + [_I64, _I64, _I64, _INT, _F, _INT, _P, _SZ, _P], _INT),
+    "gmlp_train_backward": ([_P] * 11 + [_I64, _I64, _I64, _INT, _F, _INT, _P, _SZ, _P], _INT),
 }
 
 _lib = None
@@ -106,8 +111,7 @@ def library() -> ctypes.CDLL:
 
 
 def header_functions() -> list:
-    """Names of the functions include/gmlp.h and include/softmax_matmul.h
-    declare."""
+    """Names of the functions the headers in include/ declare."""
     names = set()
     for path in HEADERS:
         text = re.sub(r"/\*.*?\*/", "", open(path).read(), flags=re.S)

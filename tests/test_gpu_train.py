@@ -1,0 +1,237 @@
+"""The Gated MLP's training step on the GPU against plain 64-bit formulas.
+
+Bounds.  Every output is an fp32 sum of products of bf16 numbers, rounded once
+to bf16 (relative error at most 2^-8 of the value; half a step).  Before that:
+
+  * G and U have no other rounding than fp32 sums of K products: an error of at
+    most K 2^-24 sum |terms|, taken as K <= 4096 terms, 2^-12 sum |terms|
+    (worst case; the sums are random).
+  * Y = H Wd with H rounded to bf16: sum |H| |Wd| 2^-8.
+  * dX, dWg, dWu: dG and dU rounded to bf16, likewise; dWd: H.
+  * act and act' in fp32: exp and rcp to 2 units in the last place, 2^-20 is ample.
+
+So each output is within  2^-8 |ref| + (2^-8 + 2^-12 + 2^-20) S (1 + 2^-8),  S the
+sum of the absolute values of its terms, with the last factor for the terms of
+second order; 1.02 * 2^-8 * S + 2^-8 |ref| covers them at the sizes used (K up to
+4096), and 2^-12 S + 2^-8 |ref| where no operand was rounded.
+"""
+import numpy as np
+import pytest
+import torch
+
+from paper_2606_26344_amd import gmlp, train
+
+pytestmark = pytest.mark.gpu
+
+HALF_STEP = 2.0 ** -8
+ROUNDED = 1.02 * 2.0 ** -8 + 2.0 ** -12
+
+
+@pytest.fixture(scope="module", autouse=True)
+def _gpu():
+    assert torch.cuda.is_available(), "GPU tests need a HIP device"
+    gmlp.library()
+
+
+def act(g, activation, beta):
+    b = beta if activation == "swish" else 1.0
+    s = torch.sigmoid(b * g)
+    if activation == "sigmoid":
+        return s, s * torch.sigmoid(-g)
+    return g * s, s + b * g * s * torch.sigmoid(-b * g)
+
+
+def inputs(T, D, F, seed):
+    gen = torch.Generator().manual_seed(seed)
+    n = lambda r, c, s: (torch.randn((r, c), generator=gen) * s).to(torch.bfloat16)  # noqa: E731
+    t = dict(x=n(T, D, 1.0), wg=n(D, F, D ** -0.5), wu=n(D, F, D ** -0.5), wd=n(F, D, F ** -0.5), dy=n(T, D, 1.0))
+    return t
+
+
+def check(name, got, ref, terms, rounded=True):
+    got = got.cpu().double()
+    assert got.shape == ref.shape, name
+    bound = HALF_STEP * ref.abs() + (ROUNDED if rounded else 2.0 ** -12) * terms + 1e-30
+    ratio = ((got - ref).abs() / bound).max().item() if ref.numel() else 0.0
+    print("%s: max |err|/bound = %.3f" % (name, ratio), flush=True)
+    assert ratio <= 1.0, name
+
+
+def run(T, D, F, activation="silu", beta=1.0, seed=0, want=train.GRADIENTS, workspace=True, data=None):
+    print("train T=%d D=%d F=%d %s want=%s" % (T, D, F, activation, want), flush=True)
+    t = data or inputs(T, D, F, seed)
+    dev = {k: v.cuda() for k, v in t.items()}
+    kw = dict(activation=activation, beta=beta, workspace=train.make_workspace(T, D, F) if workspace else None)
+    y, g, u = train.forward(dev["x"], dev["wg"], dev["wu"], dev["wd"], **kw)
+    grads = train.backward(dev["dy"], dev["x"], dev["wg"], dev["wu"], dev["wd"], g, u, want=want, **kw)
+    torch.cuda.synchronize()
+    d = {k: v.double() for k, v in t.items()}
+    check("g", g, d["x"] @ d["wg"], d["x"].abs() @ d["wg"].abs(), rounded=False)
+    check("u", u, d["x"] @ d["wu"], d["x"].abs() @ d["wu"].abs(), rounded=False)
+    # Y from the unrounded G and U.
+    ge, ue = d["x"] @ d["wg"], d["x"] @ d["wu"]
+    h = act(ge, activation, beta)[0] * ue
+    # G and U in fp32 carry up to 2^-12 of their terms into H.
+    slack = (act(ge, activation, beta)[0].abs() + 1.2 * max(1.0, beta) * ue.abs()) * 2.0 ** -12 * \
+        (d["x"].abs() @ torch.maximum(d["wg"].abs(), d["wu"].abs()))
+    check("y", y, h @ d["wd"], (h.abs() + 2.0 ** 8 * slack) @ d["wd"].abs())
+    # The backward pass from the G and U it was given.
+    gd, ud = g.cpu().double(), u.cpu().double()
+    a, da = act(gd, activation, beta)
+    dh, dh_terms = d["dy"] @ d["wd"].T, d["dy"].abs() @ d["wd"].abs().T
+    dg, du, h = dh * ud * da, dh * a, a * ud
+    # dH in fp32: 2^-12 of its terms, beside the rounding of dG and dU (2^-8).
+    dgt = dg.abs() + 2.0 ** -4 * (dh_terms * ud * da).abs()
+    dut = du.abs() + 2.0 ** -4 * (dh_terms * a).abs()
+    refs = {"dx": (dg @ d["wg"].T + du @ d["wu"].T, dgt @ d["wg"].abs().T + dut @ d["wu"].abs().T),
+            "dwg": (d["x"].T @ dg, d["x"].abs().T @ dgt), "dwu": (d["x"].T @ du, d["x"].abs().T @ dut),
+            "dwd": (h.T @ d["dy"], h.abs().T @ d["dy"].abs())}
+    for name, got in zip(train.GRADIENTS, grads):
+        if name in want:
+            check(name, got, *refs[name])
+        else:
+            assert got is None
+    return y, g, u, grads
+
+
+SHAPES = [(1, 8, 8), (1, 264, 520), (3, 264, 520), (16, 256, 512), (33, 520, 264), (64, 136, 1032), (65, 264, 264),
+          (127, 264, 1032), (130, 1032, 520), (300, 1032, 2056), (520, 264, 520)]
+
+
+@pytest.mark.parametrize("T,D,F", SHAPES, ids=["T%dD%dF%d" % s for s in SHAPES])
+def test_training_step(T, D, F):
+    run(T, D, F, seed=T * 7 + D)
+
+
+@pytest.mark.parametrize("activation,beta", [("swish", 1.702), ("sigmoid", 1.0), ("swish", -0.5)])
+@pytest.mark.parametrize("T,D,F", [(5, 264, 520), (200, 264, 520)])
+def test_activations(T, D, F, activation, beta):
+    run(T, D, F, activation, beta, seed=T)
+
+
+@pytest.mark.parametrize("T,D,F", [(260, 2048, 4096), (1029, 1288, 2312)])
+def test_large_tiles(T, D, F):
+    names = [k[0] for k in train.describe(T, D, F)]
+    assert any("<4, 2, 2, 4, 2>" in n for n in names), names
+    run(T, D, F, seed=3)
+
+
+@pytest.mark.parametrize("want", [("dx",), ("dwd",), ("dwg", "dwu"), ("dx", "dwu"), ()])
+def test_wanted_gradients_only(want):
+    run(70, 264, 520, want=want, seed=9)
+
+
+def test_without_workspace_is_bitwise_the_same():
+    a = run(130, 264, 1032, seed=4)
+    b = run(130, 264, 1032, seed=4, workspace=False)
+    for p, q in zip((*a[:3], *a[3]), (*b[:3], *b[3])):
+        assert torch.equal(p.view(torch.int16), q.view(torch.int16))
+
+
+def test_no_tokens():
+    t = {k: v.cuda() for k, v in inputs(0, 264, 520, 1).items()}
+    y, g, u = train.forward(t["x"], t["wg"], t["wu"], t["wd"])
+    assert y.shape == (0, 264) and g.shape == u.shape == (0, 520)
+    outs = [torch.full(s, 7.0, dtype=torch.bfloat16, device="cuda") for s in ((264, 520), (264, 520), (520, 264))]
+    dx, *dw = train.backward(t["dy"], t["x"], t["wg"], t["wu"], t["wd"], g, u, dwg=outs[0], dwu=outs[1], dwd=outs[2])
+    torch.cuda.synchronize()
+    assert dx.shape == (0, 264)
+    assert all(not w.any() for w in dw)
+
+
+def test_saturated_gates_have_finite_gradients():
+    # Gates of +-3e4: the sigmoid is 0 or 1, its derivative 0.
+    t = inputs(9, 264, 520, 2)
+    t["x"] = (t["x"].float() * 1e4).to(torch.bfloat16)
+    dev = {k: v.cuda() for k, v in t.items()}
+    for activation in ("silu", "sigmoid"):
+        y, g, u = train.forward(dev["x"], dev["wg"], dev["wu"], dev["wd"], activation=activation)
+        grads = train.backward(dev["dy"], dev["x"], dev["wg"], dev["wu"], dev["wd"], g, u, activation=activation)
+        assert all(torch.isfinite(v.float()).all() for v in (y, *grads))
+
+
+def test_nan_stays_in_its_token():
+    t = inputs(40, 264, 520, 6)
+    dev = {k: v.cuda() for k, v in t.items()}
+    ws = train.make_workspace(40, 264, 520)
+    y, g, u = train.forward(dev["x"], dev["wg"], dev["wu"], dev["wd"], workspace=ws)
+    clean = train.backward(dev["dy"], dev["x"], dev["wg"], dev["wu"], dev["wd"], g, u, workspace=ws)[0].clone()
+    g[17, 5] = float("nan")
+    dx = train.backward(dev["dy"], dev["x"], dev["wg"], dev["wu"], dev["wd"], g, u, want=("dx",), workspace=ws)[0]
+    rows = [i for i in range(40) if i != 17]
+    assert torch.isnan(dx[17].float()).all()
+    assert torch.equal(dx[rows].view(torch.int16), clean[rows].view(torch.int16))
+
+
+def test_gradients_against_differences():
+    # The loss sum(dy * y) in 64 bits, its directional derivatives by central
+    # differences against the kernels' gradients.
+    T, D, F = 24, 136, 264
+    t = inputs(T, D, F, 11)
+    _, g, u, grads = run(T, D, F, data=t)
+    d = {k: v.double() for k, v in t.items()}
+
+    def loss(p):
+        gg = p["x"] @ p["wg"]
+        return ((gg * torch.sigmoid(gg) * (p["x"] @ p["wu"])) @ p["wd"] * d["dy"]).sum()
+
+    gen = torch.Generator().manual_seed(5)
+    for name, got in zip(("x", "wg", "wu", "wd"), grads):
+        v = torch.randn(d[name].shape, generator=gen, dtype=torch.float64) * d[name].abs().mean()
+        eps = 1e-4
+        up, down = dict(d), dict(d)
+        up[name], down[name] = d[name] + eps * v, d[name] - eps * v
+        numeric = (loss(up) - loss(down)).item() / (2 * eps)
+        mine = (got.cpu().double() * v).sum().item()
+        # The gradient's elements are off by independent roundings of 2^-8 of
+        # their size at most, twice (dG or H, and the result), and G and U by
+        # another each; five times the root of the sum of their squares.
+        scale = (got.cpu().double() * v).norm().item()
+        assert abs(mine - numeric) <= 5 * 4 * HALF_STEP * scale + 1e-6 * abs(numeric), name
+
+
+@pytest.mark.parametrize("T,D,F", [(16, 256, 512), (200, 1032, 2056)])
+def test_captured_steps_replay(T, D, F):
+    t = {k: v.cuda() for k, v in inputs(T, D, F, 8).items()}
+    stream = torch.cuda.Stream()
+    outs = {}
+
+    def call(x):
+        y, g, u = train.forward(x, t["wg"], t["wu"], t["wd"], out=outs["y"], g=outs["g"], u=outs["u"],
+                                workspace=outs["ws"], stream=stream)
+        train.backward(t["dy"], x, t["wg"], t["wu"], t["wd"], g, u, dx=outs["dx"], dwg=outs["dwg"], dwu=outs["dwu"],
+                       dwd=outs["dwd"], workspace=outs["ws"], stream=stream)
+
+    names = {"y": (T, D), "g": (T, F), "u": (T, F), "dx": (T, D), "dwg": (D, F), "dwu": (D, F), "dwd": (F, D)}
+    torch.cuda.synchronize()
+    with torch.cuda.stream(stream):
+        outs["ws"] = train.make_workspace(T, D, F, stream=stream)
+        outs.update({k: torch.empty(s, dtype=torch.bfloat16, device="cuda") for k, s in names.items()})
+        call(t["x"])
+    torch.cuda.synchronize()
+    eager = {k: outs[k].clone() for k in names}
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=stream):
+        call(t["x"])
+    other = t["x"] * 0.5
+    torch.cuda.synchronize()
+    for i in range(4):
+        with torch.cuda.stream(stream):
+            call(other)
+            for k in names:
+                outs[k].zero_()
+            graph.replay()
+        torch.cuda.synchronize()
+        for k in names:
+            assert torch.equal(outs[k].view(torch.int16), eager[k].view(torch.int16)), (i, k)
+
+
+def test_forward_is_the_forward_of_the_inference_path():
+    # The same y as gmlp.forward up to the order of the fp32 sums.
+    T, D, F = 300, 1032, 2056
+    t = {k: v.cuda() for k, v in inputs(T, D, F, 21).items()}
+    y = train.forward(t["x"], t["wg"], t["wu"], t["wd"])[0].float()
+    z = gmlp.forward(t["x"], t["wg"], t["wu"], t["wd"]).float()
+    assert (y - z).abs().max() <= 4 * HALF_STEP * z.abs().max()
+    assert np.isfinite(y.cpu().numpy()).all()
