@@ -1,0 +1,235 @@
+// The C ABI of include/gmlp_block_norm.h: validation, launch shapes and
+// launches of the norms between two blocks (block_norm.hpp).
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "gmlp_block_norm.h"
+#include "block_norm.hpp"
+#include "hip_status.hpp"
+
+using namespace gmlp;
+
+namespace {
+
+constexpr int kNormForwardBlocks = 2048, kNormBackwardBlocks = 512;
+
+int norm_blocks(int64_t T, int most) { return (int)std::min<int64_t>(std::max<int64_t>(T, 1), most); }
+
+int check_norm_shape(int64_t T, int64_t D)
+{
+    if (T < 0 || D <= 0)
+        return fail(GMLP_ERR_INVALID_ARG, "invalid shape T=%lld D=%lld (need T >= 0, D > 0)", (long long)T, (long long)D);
+    if (D % 8)
+        return fail(GMLP_ERR_UNSUPPORTED, "D=%lld must be a multiple of 8", (long long)D);
+    if (D > GMLP_NORM_MAX_WIDTH || T > kMaxTokens || T * D > kMaxElements)
+        return fail(GMLP_ERR_UNSUPPORTED, "shape T=%lld D=%lld exceeds the supported range (D <= %d, T <= %lld, at most "
+                    "%lld elements per tensor)", (long long)T, (long long)D, GMLP_NORM_MAX_WIDTH, (long long)kMaxTokens,
+                    (long long)kMaxElements);
+    return GMLP_OK;
+}
+
+// has_y: Y is given (or has no rows).
+int check_norm_args(int flags, float res_scale, float eps, bool has_y, const void *w_post, const void *gate)
+{
+    if (flags & ~(GMLP_NORM_POST | GMLP_NORM_RES_FP32 | GMLP_NORM_GATE_ROWS))
+        return fail(GMLP_ERR_INVALID_ARG, "unknown flags %d", flags);
+    if (!std::isfinite(res_scale) || !(std::isfinite(eps) && eps >= 0.0f))
+        return fail(GMLP_ERR_INVALID_ARG, "res_scale must be finite, eps finite and >= 0");
+    if (w_post && !(flags & GMLP_NORM_POST))
+        return fail(GMLP_ERR_INVALID_ARG, "w_post without GMLP_NORM_POST");
+    if ((flags & GMLP_NORM_GATE_ROWS) && !gate)
+        return fail(GMLP_ERR_INVALID_ARG, "GMLP_NORM_GATE_ROWS without a gate");
+    if (!has_y && ((flags & GMLP_NORM_POST) || gate))
+        return fail(GMLP_ERR_INVALID_ARG, "a norm after the block or a gate without Y");
+    return GMLP_OK;
+}
+
+struct NormSpan {
+    const void *p;
+    size_t bytes;
+    const char *name;
+    const void *same; // an output may be this input itself
+};
+
+int check_norm_spans(const NormSpan *in, int n_in, const NormSpan *out, int n_out, const void *ws, size_t ws_bytes)
+{
+    for (int i = 0; i < n_out; ++i) {
+        if (!out[i].p)
+            continue;
+        for (int j = 0; j < n_in; ++j)
+            if (in[j].p && overlaps(out[i].p, out[i].bytes, in[j].p, in[j].bytes) &&
+                !(in[j].p == out[i].p && out[i].same == in[j].p && out[i].bytes == in[j].bytes))
+                return fail(GMLP_ERR_INVALID_ARG, "%s overlaps %s", out[i].name, in[j].name);
+        for (int j = 0; j < i; ++j)
+            if (out[j].p && overlaps(out[i].p, out[i].bytes, out[j].p, out[j].bytes))
+                return fail(GMLP_ERR_INVALID_ARG, "%s overlaps %s", out[i].name, out[j].name);
+        if (ws && overlaps(out[i].p, out[i].bytes, ws, ws_bytes))
+            return fail(GMLP_ERR_INVALID_ARG, "%s overlaps the workspace", out[i].name);
+    }
+    return GMLP_OK;
+}
+
+// f(threads, chunks) as integral constants for a row of D elements.
+template <class F>
+int with_norm_shape(int64_t D, F f)
+{
+    using std::integral_constant;
+    const int64_t chunks = D / 8;
+    if (chunks <= 64)
+        return f(integral_constant<int, 64>{}, integral_constant<int, 1>{});
+    if (chunks <= 128)
+        return f(integral_constant<int, 64>{}, integral_constant<int, 2>{});
+    if (chunks <= 256)
+        return f(integral_constant<int, 128>{}, integral_constant<int, 2>{});
+    if (chunks <= 512)
+        return f(integral_constant<int, 256>{}, integral_constant<int, 2>{});
+    if (chunks <= 1024)
+        return f(integral_constant<int, 512>{}, integral_constant<int, 2>{});
+    if (chunks <= 2048)
+        return f(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
+    return f(integral_constant<int, 1024>{}, integral_constant<int, 4>{});
+}
+
+NormParams norm_params(const void *y, const void *res, const void *w_pre, const void *w_post, const void *gate,
+                       int64_t T, int64_t D, int flags, float res_scale, float eps)
+{
+    NormParams p{};
+    p.y = static_cast<const uint16_t *>(y);
+    p.res = res;
+    p.w_pre = static_cast<const uint16_t *>(w_pre);
+    p.w_post = static_cast<const uint16_t *>(w_post);
+    p.gate = static_cast<const uint16_t *>(gate);
+    p.gate_stride = flags & GMLP_NORM_GATE_ROWS ? (size_t)D : 0;
+    p.T = (int)T;
+    p.D = (int)D;
+    p.post = flags & GMLP_NORM_POST ? 1 : 0;
+    p.res_scale = res_scale;
+    p.eps = eps;
+    return p;
+}
+
+} // namespace
+
+extern "C" {
+
+int gmlp_block_norm(const void *Y, const void *res, const void *w_pre, const void *w_post, const void *gate, void *R,
+                    void *Xn, int64_t T, int64_t D, int flags, float res_scale, float eps, void *stream)
+{
+    int rc;
+    const bool rows = T > 0;
+    const bool gate_rows = flags & GMLP_NORM_GATE_ROWS;
+    if ((rc = check_norm_shape(T, D)) ||
+        (rows && (rc = check_norm_args(flags, res_scale, eps, Y, w_post, gate))) || (rc = check_ptr(Y, "Y", false)) || (rc = check_ptr(res, "res", rows)) || (rc = check_ptr(w_pre, "w_pre", false)) ||
+        (rc = check_ptr(w_post, "w_post", false)) || (rc = check_ptr(gate, "gate", false)) ||
+        (rc = check_ptr(R, "R", rows && Y)) || (rc = check_ptr(Xn, "Xn", rows)))
+        return rc;
+    if (!rows)
+        return ok();
+    const size_t b = flags & GMLP_NORM_RES_FP32 ? 4 : 2, e = (size_t)T * D;
+    const NormSpan in[] = {{Y, 2 * e, "Y", nullptr}, {res, b * e, "res", nullptr}, {w_pre, 2 * (size_t)D, "w_pre", nullptr},
+                           {w_post, 2 * (size_t)D, "w_post", nullptr},
+                           {gate, 2 * (gate_rows ? e : (size_t)D), "gate", nullptr}};
+    const NormSpan out[] = {{R, b * e, "R", res}, {Xn, 2 * e, "Xn", Y}};
+    if ((rc = check_norm_spans(in, 5, out, 2, nullptr, 0)))
+        return rc;
+    NormParams p = norm_params(Y, res, w_pre, w_post, gate, T, D, flags, res_scale, eps);
+    p.r_out = R;
+    p.xn = static_cast<uint16_t *>(Xn);
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    rc = with_norm_shape(D, [&](auto threads, auto chunks) {
+        constexpr int NT = decltype(threads)::value, CH = decltype(chunks)::value;
+        const dim3 grid(norm_blocks(T, kNormForwardBlocks)), block(NT);
+        if (flags & GMLP_NORM_RES_FP32)
+            hipLaunchKernelGGL((norm_forward_kernel<NT, CH, true>), grid, block, 0, st, p);
+        else
+            hipLaunchKernelGGL((norm_forward_kernel<NT, CH, false>), grid, block, 0, st, p);
+        return hip_check(hipGetLastError(), "norm launch");
+    });
+    return rc ? rc : ok();
+}
+
+size_t gmlp_block_norm_workspace_size(int64_t T, int64_t D)
+{
+    if (check_norm_shape(T, D))
+        return 0;
+    return align_up((size_t)3 * norm_blocks(T, kNormBackwardBlocks) * D * sizeof(float));
+}
+
+int gmlp_block_norm_backward(const void *dXn, const void *dR, const void *Y, const void *R, const void *w_pre,
+                             const void *w_post, const void *gate, void *dY, void *dres, void *dw_pre, void *dw_post,
+                             void *dgate, int64_t T, int64_t D, int flags, float res_scale, float eps, void *workspace,
+                             size_t ws_bytes, void *stream)
+{
+    int rc;
+    const bool rows = T > 0, gate_rows = flags & GMLP_NORM_GATE_ROWS;
+    if ((rc = check_norm_shape(T, D)) ||
+        (rows && (rc = check_norm_args(flags, res_scale, eps, Y, w_post, gate))) || (rc = check_ptr(dXn, "dXn", rows)) || (rc = check_ptr(dR, "dR", false)) || (rc = check_ptr(Y, "Y", false)) ||
+        (rc = check_ptr(R, "R", rows)) || (rc = check_ptr(w_pre, "w_pre", false)) ||
+        (rc = check_ptr(w_post, "w_post", false)) || (rc = check_ptr(gate, "gate", false)) ||
+        (rc = check_ptr(dY, "dY", false)) || (rc = check_ptr(dres, "dres", false)) ||
+        (rc = check_ptr(dw_pre, "dw_pre", false)) || (rc = check_ptr(dw_post, "dw_post", false)) ||
+        (rc = check_ptr(dgate, "dgate", false)))
+        return rc;
+    if (dw_pre && !w_pre)
+        return fail(GMLP_ERR_INVALID_ARG, "dw_pre without w_pre");
+    if (dw_post && !w_post)
+        return fail(GMLP_ERR_INVALID_ARG, "dw_post without w_post");
+    if (dgate && !gate)
+        return fail(GMLP_ERR_INVALID_ARG, "dgate without a gate");
+    if (rows && dY && !Y)
+        return fail(GMLP_ERR_INVALID_ARG, "dY without Y");
+    const int sums = (dw_pre ? 1 : 0) | (dw_post ? 2 : 0) | (dgate && !gate_rows ? 4 : 0);
+    const size_t need = gmlp_block_norm_workspace_size(T, D);
+    if (sums) {
+        if (!workspace)
+            return fail(GMLP_ERR_INVALID_ARG, "workspace is NULL");
+        if (reinterpret_cast<uintptr_t>(workspace) % kAlign)
+            return fail(GMLP_ERR_UNSUPPORTED, "workspace %p is not %zu-byte aligned", workspace, kAlign);
+        if (ws_bytes < need)
+            return fail(GMLP_ERR_NO_MEMORY, "workspace of %zu bytes, %zu needed", ws_bytes, need);
+    }
+    const size_t b = flags & GMLP_NORM_RES_FP32 ? 4 : 2, e = (size_t)T * D, d = 2 * (size_t)D;
+    const NormSpan in[] = {{dXn, 2 * e, "dXn", nullptr}, {dR, b * e, "dR", nullptr}, {Y, 2 * e, "Y", nullptr},
+                           {R, b * e, "R", nullptr},     {w_pre, d, "w_pre", nullptr}, {w_post, d, "w_post", nullptr},
+                           {gate, gate_rows ? 2 * e : d, "gate", nullptr}};
+    const NormSpan out[] = {{dY, 2 * e, "dY", dXn}, {dres, b * e, "dres", dR}, {dw_pre, d, "dw_pre", nullptr},
+                            {dw_post, d, "dw_post", nullptr}, {dgate, gate_rows ? 2 * e : d, "dgate", nullptr}};
+    if ((rc = check_norm_spans(in, 7, out, 5, sums ? workspace : nullptr, need)))
+        return rc;
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    const int blocks = norm_blocks(T, kNormBackwardBlocks);
+    float *partial = static_cast<float *>(workspace);
+    if (rows && (dY || dres || sums || dgate)) {
+        NormParams p = norm_params(Y, R, w_pre, w_post, gate, T, D, flags, res_scale, eps);
+        p.dxn = static_cast<const uint16_t *>(dXn);
+        p.dr = dR;
+        p.dy = static_cast<uint16_t *>(dY);
+        p.dres = dres;
+        p.dgate = gate_rows ? static_cast<uint16_t *>(dgate) : nullptr;
+        p.partial = partial;
+        p.sums = sums;
+        rc = with_norm_shape(D, [&](auto threads, auto chunks) {
+            constexpr int NT = decltype(threads)::value, CH = decltype(chunks)::value;
+            if (flags & GMLP_NORM_RES_FP32)
+                hipLaunchKernelGGL((norm_backward_kernel<NT, CH, true>), dim3(blocks), dim3(NT), 0, st, p);
+            else
+                hipLaunchKernelGGL((norm_backward_kernel<NT, CH, false>), dim3(blocks), dim3(NT), 0, st, p);
+            return hip_check(hipGetLastError(), "norm backward launch");
+        });
+        if (rc)
+            return rc;
+    }
+    if (sums) {
+        hipLaunchKernelGGL(norm_columns_kernel, dim3((unsigned)cdiv(D, kNormColumns), 3),
+                           dim3(kNormColumns * kNormGroups), 0, st, partial, static_cast<uint16_t *>(dw_pre),
+                           static_cast<uint16_t *>(dw_post), sums & 4 ? static_cast<uint16_t *>(dgate) : nullptr,
+                           rows ? blocks : 0, (int)D);
+        if ((rc = hip_check(hipGetLastError(), "norm column sums launch")))
+            return rc;
+    }
+    return ok();
+}
+
+} // extern "C"

@@ -1,6 +1,5 @@
-// Launch helpers shared by the host code of libgmlp.so: HIP errors as status
-// codes, GEMM parameters and launches, and the counters of a workspace that has
-// not been prepared.
+// Launch helpers of the GEMM kernels: their parameters and launches, and the
+// counters of a workspace that has not been prepared.
 #pragma once
 
 #include <hip/hip_runtime.h>
@@ -8,17 +7,11 @@
 #include <algorithm>
 
 #include "gemm_mfma.hpp"
+#include "hip_status.hpp"
 #include "plan.hpp"
 
 namespace gmlp {
 namespace {
-
-inline int hip_check(hipError_t e, const char *what)
-{
-    if (e != hipSuccess)
-        return fail(GMLP_ERR_HIP, "%s: %s", what, hipGetErrorString(e));
-    return GMLP_OK;
-}
 
 inline GemmParams gemm_params(const Step &s, const void *w0, const void *w1, const void *act, void *out, uint8_t *ws,
                        const Layout &l, const Variant &v, const float *rrms, const float *rowdiv)

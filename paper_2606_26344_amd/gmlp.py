@@ -34,7 +34,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIBRARY = os.path.join(HERE, "libgmlp.so")
 HEADER = os.path.join(os.path.dirname(HERE), "include", "gmlp.h")
 HEADERS = [os.path.join(os.path.dirname(HERE), "include", h)
-           for h in ("gmlp.h", "softmax_matmul.h", "gmlp_train.h")]
+           for h in ("gmlp.h", "softmax_matmul.h", "gmlp_train.h", "gmlp_block_norm.h")]
 
 PATH_AUTO, PATH_GEMV, PATH_MFMA, PATH_FUSED, PATH_FUSED_MFMA = 0, 1, 2, 3, 4
 _PATHS = {"auto": PATH_AUTO, "gemv": PATH_GEMV, "mfma": PATH_MFMA, "fused": PATH_FUSED,
@@ -84,6 +84,9 @@ _SIGNATURES = {
     "gmlp_train_describe": ([_I64, _I64, _I64, _INT, ctypes.c_char_p, _SZ], _INT),
     "gmlp_train_forward": ([_P] * 7 + [_I64, _I64, _I64, _INT, _F, _INT, _P, _SZ, _P], _INT),
     "gmlp_train_backward": ([_P] * 11 + [_I64, _I64, _I64, _INT, _F, _INT, _P, _SZ, _P], _INT),
+    "gmlp_block_norm": ([_P] * 7 + [_I64, _I64, _INT, _F, _F, _P], _INT),
+    "gmlp_block_norm_workspace_size": ([_I64, _I64], _SZ),
+    "gmlp_block_norm_backward": ([_P] * 12 + [_I64, _I64, _INT, _F, _F, _P, _SZ, _P], _INT),
 }
 
 _lib = None
