@@ -1,0 +1,309 @@
+// The C ABI of include/gmlp_w4.h: validation and launches of the products with
+// 4-bit weights (w4.hpp).
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cmath>
+
+#include "gmlp_w4.h"
+#include "hip_status.hpp"
+#include "w4.hpp"
+
+using namespace gmlp;
+
+namespace {
+
+// Where the parts of a packed weight lie.
+struct W4Packed {
+    int64_t ktiles = 0, ntiles = 0;
+    size_t scales = 0, zeros = 0, total = 0;
+};
+
+W4Packed w4_packed(int64_t K, int64_t N, int group, int zeros)
+{
+    W4Packed l;
+    l.ktiles = cdiv(K, 128);
+    l.ntiles = cdiv(N, 16);
+    const size_t groups = (size_t)l.ktiles * l.ntiles * 16 * (128 / group);
+    l.scales = (size_t)l.ktiles * l.ntiles * 1024;
+    l.zeros = l.scales + align_up(groups * 2);
+    l.total = l.zeros + (zeros ? align_up(groups) : 0);
+    return l;
+}
+
+int check_w4_weight(int64_t K, int64_t N, int group)
+{
+    int rc;
+    if ((rc = check_smm_shape(0, K, N)))
+        return rc;
+    if (group != 32 && group != 64 && group != 128)
+        return fail(GMLP_ERR_UNSUPPORTED, "groups of 32, 64 or 128 rows (got %d)", group);
+    return GMLP_OK;
+}
+
+int check_w4_tokens(int64_t T)
+{
+    if (T < 0)
+        return fail(GMLP_ERR_INVALID_ARG, "invalid T=%lld", (long long)T);
+    if (T > GMLP_W4_MAX_TOKENS)
+        return fail(GMLP_ERR_UNSUPPORTED, "%lld tokens: at most %d (gmlp_w4_dequantize gives the weight for more)",
+                    (long long)T, GMLP_W4_MAX_TOKENS);
+    return GMLP_OK;
+}
+
+int check_w4_packed(const void *p, const char *name)
+{
+    int rc;
+    if ((rc = check_ptr(p, name, true)))
+        return rc;
+    if (reinterpret_cast<uintptr_t>(p) % kAlign)
+        return fail(GMLP_ERR_UNSUPPORTED, "%s (%p) is not %zu-byte aligned", name, p, kAlign);
+    return GMLP_OK;
+}
+
+int check_w4_path(int path)
+{
+    return path == GMLP_PATH_AUTO || path == (GMLP_PATH_AUTO | GMLP_FRESH_WORKSPACE)
+               ? GMLP_OK
+               : fail(GMLP_ERR_INVALID_ARG, "4-bit products have the automatic path only (got %d)", path);
+}
+
+// The counter block of every workspace, then H [T, F].
+size_t w4_workspace(int64_t T, int64_t D, int64_t F) { return kCounterBytes + align_up((size_t)std::max<int64_t>(T, 1) * std::max(D, F) * 2); }
+
+int check_w4_workspace(void *ws, size_t bytes, size_t need)
+{
+    if (!ws)
+        return fail(GMLP_ERR_INVALID_ARG, "workspace is NULL");
+    if (reinterpret_cast<uintptr_t>(ws) % kAlign)
+        return fail(GMLP_ERR_UNSUPPORTED, "workspace %p is not %zu-byte aligned", ws, kAlign);
+    if (bytes < need)
+        return fail(GMLP_ERR_NO_MEMORY, "workspace of %zu bytes, %zu needed", bytes, need);
+    return GMLP_OK;
+}
+
+constexpr int kW4Waves = 8;
+
+template <int TOK, int NW, int CT, int GPT, bool ZEROS>
+int launch_w4(const W4Params &p, hipStream_t st)
+{
+    constexpr int DEPTH = TOK > 32 ? 1 : TOK > 16 ? 2 : NW * CT >= 4 ? 2 : NW * CT == 2 ? 3 : 4;
+    hipLaunchKernelGGL((w4_kernel<TOK, NW, CT, GPT, ZEROS, kW4Waves, DEPTH>), dim3((unsigned)cdiv(p.N, 16 * CT)),
+                       dim3(kW4Waves * 64), 0, st, p);
+    return hip_check(hipGetLastError(), "4-bit product launch");
+}
+
+template <int TOK, int NW, int GPT, bool ZEROS>
+int launch_w4_width(const W4Params &p, hipStream_t st)
+{
+    if constexpr (NW == 1)
+        if (cdiv(p.N, 32) < kBlockTarget)
+            return launch_w4<TOK, 1, 1, GPT, ZEROS>(p, st);
+    return launch_w4<TOK, NW, 2, GPT, ZEROS>(p, st);
+}
+
+template <int TOK, int NW>
+int launch_w4_group(const W4Params &p, int group, bool zeros, hipStream_t st)
+{
+    switch (group) {
+    case 32: return zeros ? launch_w4_width<TOK, NW, 4, true>(p, st) : launch_w4_width<TOK, NW, 4, false>(p, st);
+    case 64: return zeros ? launch_w4_width<TOK, NW, 2, true>(p, st) : launch_w4_width<TOK, NW, 2, false>(p, st);
+    default: return zeros ? launch_w4_width<TOK, NW, 1, true>(p, st) : launch_w4_width<TOK, NW, 1, false>(p, st);
+    }
+}
+
+template <int NW>
+int run_w4(const void *X, const void *const (&packed)[2], void *out, int64_t T, int64_t K, int64_t N, int group, bool zeros,
+           int activation, float beta, hipStream_t st)
+{
+    const W4Packed l = w4_packed(K, N, group, zeros);
+    W4Params p{};
+    p.x = static_cast<const uint16_t *>(X);
+    for (int w = 0; w < NW; ++w) {
+        p.tiles[w] = static_cast<const uint8_t *>(packed[w]);
+        p.scales[w] = p.tiles[w] + l.scales;
+        p.zeros[w] = p.tiles[w] + l.zeros;
+    }
+    p.out = static_cast<uint16_t *>(out);
+    p.T = (int)T;
+    p.K = (int)K;
+    p.N = (int)N;
+    p.ktiles = (int)l.ktiles;
+    p.activation = activation;
+    p.beta = beta;
+    if (T <= 4)
+        return launch_w4_group<4, NW>(p, group, zeros, st);
+    if (T <= 16)
+        return launch_w4_group<16, NW>(p, group, zeros, st);
+    if (T <= 32)
+        return launch_w4_group<32, NW>(p, group, zeros, st);
+    return launch_w4_group<64, NW>(p, group, zeros, st);
+}
+
+W4LayoutParams w4_layout_params(void *packed, int64_t K, int64_t N, int group, int zeros)
+{
+    const W4Packed l = w4_packed(K, N, group, zeros);
+    W4LayoutParams p{};
+    p.tiles = static_cast<uint8_t *>(packed);
+    p.scales = p.tiles + l.scales;
+    p.zeros = zeros ? p.tiles + l.zeros : nullptr;
+    p.K = (int)K;
+    p.N = (int)N;
+    p.group = group;
+    p.ktiles = (int)l.ktiles;
+    p.ntiles = (int)l.ntiles;
+    return p;
+}
+
+unsigned w4_layout_blocks(const W4LayoutParams &p) { return (unsigned)cdiv((int64_t)p.ktiles * p.ntiles, 4); }
+
+} // namespace
+
+extern "C" {
+
+size_t gmlp_w4_packed_size(int64_t K, int64_t N, int group, int zeros)
+{
+    if (check_w4_weight(K, N, group))
+        return 0;
+    return w4_packed(K, N, group, zeros).total;
+}
+
+int gmlp_w4_quantize(const void *W, void *Q, void *S, void *Z, int64_t K, int64_t N, int group, void *stream)
+{
+    int rc;
+    if ((rc = check_w4_weight(K, N, group)) || (rc = check_ptr(W, "W", true)) || (rc = check_ptr(Q, "Q", true)) ||
+        (rc = check_ptr(S, "S", true)) || (rc = check_ptr(Z, "Z", false)))
+        return rc;
+    const size_t n = (size_t)K * N, g = (size_t)cdiv(K, group) * N;
+    if (overlaps(Q, n, W, 2 * n) || overlaps(S, 2 * g, W, 2 * n) || overlaps(S, 2 * g, Q, n) ||
+        (Z && (overlaps(Z, g, W, 2 * n) || overlaps(Z, g, Q, n) || overlaps(Z, g, S, 2 * g))))
+        return fail(GMLP_ERR_INVALID_ARG, "W, Q, S and Z must not overlap");
+    W4LayoutParams p{};
+    p.w = const_cast<uint16_t *>(static_cast<const uint16_t *>(W));
+    p.q = static_cast<uint8_t *>(Q);
+    p.s = static_cast<uint16_t *>(S);
+    p.z = static_cast<uint8_t *>(Z);
+    p.K = (int)K;
+    p.N = (int)N;
+    p.group = group;
+    hipLaunchKernelGGL(w4_quantize_kernel, dim3((unsigned)(cdiv(N, 256) * cdiv(K, group))), dim3(256), 0,
+                       static_cast<hipStream_t>(stream), p);
+    rc = hip_check(hipGetLastError(), "quantise launch");
+    return rc ? rc : ok();
+}
+
+int gmlp_w4_pack(const void *Q, const void *S, const void *Z, void *packed, int64_t K, int64_t N, int group, void *stream)
+{
+    int rc;
+    if ((rc = check_w4_weight(K, N, group)) || (rc = check_ptr(Q, "Q", true)) || (rc = check_ptr(S, "S", true)) ||
+        (rc = check_ptr(Z, "Z", false)) || (rc = check_w4_packed(packed, "packed")))
+        return rc;
+    const size_t n = (size_t)K * N, g = (size_t)cdiv(K, group) * N, b = w4_packed(K, N, group, Z != nullptr).total;
+    if (overlaps(packed, b, Q, n) || overlaps(packed, b, S, 2 * g) || (Z && overlaps(packed, b, Z, g)))
+        return fail(GMLP_ERR_INVALID_ARG, "packed overlaps an input");
+    W4LayoutParams p = w4_layout_params(packed, K, N, group, Z != nullptr);
+    p.q = const_cast<uint8_t *>(static_cast<const uint8_t *>(Q));
+    p.s = const_cast<uint16_t *>(static_cast<const uint16_t *>(S));
+    p.z = const_cast<uint8_t *>(static_cast<const uint8_t *>(Z));
+    hipLaunchKernelGGL(w4_pack_kernel, dim3(w4_layout_blocks(p)), dim3(256), 0, static_cast<hipStream_t>(stream), p);
+    rc = hip_check(hipGetLastError(), "pack launch");
+    return rc ? rc : ok();
+}
+
+int gmlp_w4_dequantize(const void *packed, void *W, int64_t K, int64_t N, int group, int zeros, void *stream)
+{
+    int rc;
+    if ((rc = check_w4_weight(K, N, group)) || (rc = check_w4_packed(packed, "packed")) || (rc = check_ptr(W, "W", true)))
+        return rc;
+    if (overlaps(W, 2 * (size_t)K * N, packed, w4_packed(K, N, group, zeros).total))
+        return fail(GMLP_ERR_INVALID_ARG, "W overlaps packed");
+    W4LayoutParams p = w4_layout_params(const_cast<void *>(packed), K, N, group, zeros);
+    p.w = static_cast<uint16_t *>(W);
+    hipLaunchKernelGGL(w4_dequantize_kernel, dim3(w4_layout_blocks(p)), dim3(256), 0, static_cast<hipStream_t>(stream), p);
+    rc = hip_check(hipGetLastError(), "dequantise launch");
+    return rc ? rc : ok();
+}
+
+size_t gmlp_w4_workspace_size(int64_t T, int64_t D, int64_t F)
+{
+    if (check_w4_tokens(T) || check_smm_shape(0, D, F))
+        return 0;
+    return w4_workspace(T, D, F);
+}
+
+int gmlp_w4_matmul(const void *X, const void *packed, void *Y, int64_t T, int64_t K, int64_t N, int group, int zeros,
+                   int path, void *workspace, size_t ws_bytes, void *stream)
+{
+    int rc;
+    const bool rows = T > 0;
+    if ((rc = check_w4_tokens(T)) || (rc = check_w4_weight(K, N, group)) || (rc = check_ptr(X, "X", rows)) ||
+        (rc = check_w4_packed(packed, "packed")) || (rc = check_ptr(Y, "Y", rows)) || (rc = check_w4_path(path)))
+        return rc;
+    if (!rows)
+        return ok();
+    const size_t need = w4_workspace(T, K, N), yb = 2 * (size_t)T * N;
+    if ((rc = check_w4_workspace(workspace, ws_bytes, need)))
+        return rc;
+    if (overlaps(Y, yb, X, 2 * (size_t)T * K) || overlaps(Y, yb, packed, w4_packed(K, N, group, zeros).total) ||
+        overlaps(Y, yb, workspace, need))
+        return fail(GMLP_ERR_INVALID_ARG, "Y overlaps an input or the workspace");
+    const void *const w[2] = {packed, nullptr};
+    rc = run_w4<1>(X, w, Y, T, K, N, group, zeros, 0, 1.0f, static_cast<hipStream_t>(stream));
+    return rc ? rc : ok();
+}
+
+int gmlp_w4_gate_up(const void *X, const void *packed_g, const void *packed_u, void *H, int64_t T, int64_t D, int64_t F,
+                    int group, int zeros, int activation, float beta, int path, void *workspace, size_t ws_bytes,
+                    void *stream)
+{
+    int rc;
+    Variant v;
+    const bool rows = T > 0;
+    if ((rc = check_w4_tokens(T)) || (rc = check_w4_weight(D, F, group)) || (rc = check_ptr(X, "X", rows)) ||
+        (rc = check_w4_packed(packed_g, "packed_g")) || (rc = check_w4_packed(packed_u, "packed_u")) ||
+        (rc = check_ptr(H, "H", rows)) || (rc = check_w4_path(path)) || (rc = check_variant(activation, beta, 0, 0.0f, &v)))
+        return rc;
+    if (!rows)
+        return ok();
+    const size_t need = w4_workspace(T, D, F), hb = 2 * (size_t)T * F, pb = w4_packed(D, F, group, zeros).total;
+    if ((rc = check_w4_workspace(workspace, ws_bytes, need)))
+        return rc;
+    if (overlaps(H, hb, X, 2 * (size_t)T * D) || overlaps(H, hb, packed_g, pb) || overlaps(H, hb, packed_u, pb) ||
+        overlaps(H, hb, workspace, need))
+        return fail(GMLP_ERR_INVALID_ARG, "H overlaps an input or the workspace");
+    const void *const w[2] = {packed_g, packed_u};
+    rc = run_w4<2>(X, w, H, T, D, F, group, zeros, v.act, v.beta, static_cast<hipStream_t>(stream));
+    return rc ? rc : ok();
+}
+
+int gmlp_w4_forward(const void *X, const void *packed_g, const void *packed_u, const void *packed_d, void *Y, int64_t T,
+                    int64_t D, int64_t F, int group, int zeros, int activation, float beta, int path, void *workspace,
+                    size_t ws_bytes, void *stream)
+{
+    int rc;
+    Variant v;
+    const bool rows = T > 0;
+    if ((rc = check_w4_tokens(T)) || (rc = check_w4_weight(D, F, group)) || (rc = check_ptr(X, "X", rows)) ||
+        (rc = check_w4_packed(packed_g, "packed_g")) || (rc = check_w4_packed(packed_u, "packed_u")) ||
+        (rc = check_w4_packed(packed_d, "packed_d")) || (rc = check_ptr(Y, "Y", rows)) || (rc = check_w4_path(path)) ||
+        (rc = check_variant(activation, beta, 0, 0.0f, &v)))
+        return rc;
+    if (!rows)
+        return ok();
+    const size_t need = w4_workspace(T, D, F), yb = 2 * (size_t)T * D;
+    const size_t gb = w4_packed(D, F, group, zeros).total, db = w4_packed(F, D, group, zeros).total;
+    if ((rc = check_w4_workspace(workspace, ws_bytes, need)))
+        return rc;
+    if (overlaps(Y, yb, X, 2 * (size_t)T * D) || overlaps(Y, yb, packed_g, gb) || overlaps(Y, yb, packed_u, gb) ||
+        overlaps(Y, yb, packed_d, db) || overlaps(Y, yb, workspace, need))
+        return fail(GMLP_ERR_INVALID_ARG, "Y overlaps an input or the workspace");
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    void *H = static_cast<uint8_t *>(workspace) + kCounterBytes;
+    const void *const gu[2] = {packed_g, packed_u}, *const dn[2] = {packed_d, nullptr};
+    if ((rc = run_w4<2>(X, gu, H, T, D, F, group, zeros, v.act, v.beta, st)) ||
+        (rc = run_w4<1>(H, dn, Y, T, F, D, group, zeros, 0, 1.0f, st)))
+        return rc;
+    return ok();
+}
+
+} // extern "C"

@@ -1,0 +1,327 @@
+// Products with 4-bit weights (include/gmlp_w4.h) for gfx950.
+//
+// Y[t, n] = sum_k X[t, k] (q[k, n] - z) s for few tokens t, bound by the bytes of
+// q.  The arithmetic follows from making the matrix cores do all of it:
+//
+//   * A 4-bit q in the low mantissa bits of a bf16 one is the bf16 number
+//     1 + q / 128, exactly: one v_and_or_b32 makes two weights, 7 VALU
+//     instructions 8 of them.
+//   * sum x (q - z) / 128 = sum x (1 + q / 128) - sum x (1 + z / 128).  The second
+//     sum is an MFMA with a constant operand; its result is the accumulator the
+//     first starts from.  Without zero points (z = 8) it is shared by all columns.
+//   * v_mfma_f32_16x16x32_bf16 with X as operand A (16 tokens) and the weights as
+//     B: a lane then holds results of one column, so a group's scale is one
+//     number per lane and one FMA per result.  Tokens sit at rows 0, 4, 8, 12, 1,
+//     5, ...: up to 4 tokens use one result register of the four.
+//
+// Packed layout: tiles of 128 rows x 16 columns, 1 KB each, k-tiles of a column
+// tile consecutive.  Lane l of a wave reads 16 bytes, column l % 16; its dword j
+// holds rows 32 j + 8 (l / 16) .. + 7, the operand of MFMA j, row e in bits
+// 4 (e / 2) + 16 (e % 2).  So a wave streams 1 KB per load, in order, straight
+// into registers.  Scales [tile][column][group of the tile], zero points likewise.
+//
+// A block of WAVES waves computes CT column tiles (of both weights for gate/up),
+// each wave a contiguous range of the k-tiles; the waves' sums are added in
+// order through LDS.
+#pragma once
+
+#include "common.hpp"
+
+namespace gmlp {
+
+struct W4Params {
+    const uint16_t *x;       // [T, K]
+    const uint8_t *tiles[2]; // packed weights
+    const uint8_t *scales[2], *zeros[2];
+    uint16_t *out;           // [T, N]
+    int T, K, N;
+    int ktiles;              // tiles of 128 rows
+    int activation;
+    float beta;
+};
+
+constexpr uint32_t kW4Nibbles = 0x000f000fu, kW4One = 0x3f803f80u;
+constexpr uint32_t kW4MinusMid = 0xbf88bf88u; // -(1 + 8 / 128), twice
+
+// The k-tile's scales (or zero points) of one column, G of them.
+template <int G>
+struct W4Group;
+template <>
+struct W4Group<1> {
+    typedef uint16_t scales;
+    typedef uint8_t zeros;
+    __device__ static uint32_t scale(scales s, int) { return (uint32_t)s << 16; }
+    __device__ static uint32_t zero(zeros z, int) { return z; }
+};
+template <>
+struct W4Group<2> {
+    typedef uint32_t scales;
+    typedef uint16_t zeros;
+    __device__ static uint32_t scale(scales s, int g) { return g ? s & 0xffff0000u : s << 16; }
+    __device__ static uint32_t zero(zeros z, int g) { return z >> (8 * g) & 0xffu; }
+};
+template <>
+struct W4Group<4> {
+    typedef u32x2 scales;
+    typedef uint32_t zeros;
+    __device__ static uint32_t scale(const scales &s, int g) { return g & 1 ? s[g >> 1] & 0xffff0000u : s[g >> 1] << 16; }
+    __device__ static uint32_t zero(zeros z, int g) { return z >> (8 * g) & 0xffu; }
+};
+
+// Eight weights 1 + q / 128 of one packed dword.
+__device__ __forceinline__ bf16x8 w4_unpack(uint32_t d)
+{
+    return __builtin_bit_cast(bf16x8, u32x4{(d & kW4Nibbles) | kW4One, (d >> 4 & kW4Nibbles) | kW4One,
+                                            (d >> 8 & kW4Nibbles) | kW4One, (d >> 12 & kW4Nibbles) | kW4One});
+}
+
+// TOK: tokens, rounded up to 4, 16, 32 or 64.  GPT: groups per k-tile (128 /
+// group).  DEPTH: k-tiles of a wave in flight.
+template <int TOK, int NW, int CT, int GPT, bool ZEROS, int WAVES, int DEPTH>
+__global__ __launch_bounds__(WAVES * 64) void w4_kernel(W4Params p)
+{
+    constexpr int NB = (TOK + 15) / 16, NR = TOK >= 16 ? 4 : TOK / 4, MPG = 4 / GPT;
+    constexpr int SLOTS = NW * CT * NB * NR;
+    using Group = W4Group<GPT>;
+    __shared__ float part[WAVES * SLOTS * 64];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int K = p.K, ktiles = p.ktiles;
+    const int ntiles = (p.N + 15) >> 4;
+    const int first = blockIdx.x * CT;
+    const int per = (ktiles + WAVES - 1) / WAVES;
+    const int begin = wave * per, end = min(ktiles, begin + per);
+
+    // Row r of operand A is token r / 4 + 4 (r % 4) of its 16; tokens past T
+    // repeat the last one and feed results that are not stored.
+    const __amdgpu_buffer_rsrc_t rx = make_rsrc(p.x);
+    const int kq = lane >> 4, row = lane & 15;
+    uint32_t x_off[NB];
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+        x_off[nb] = ((uint32_t)min(16 * nb + (row >> 2) + 4 * (row & 3), p.T - 1) * (uint32_t)K + 8u * kq) * 2u;
+    size_t tile[CT];
+#pragma unroll
+    for (int c = 0; c < CT; ++c)
+        tile[c] = (size_t)min(first + c, ntiles - 1) * ktiles;
+
+    struct Batch {
+        u32x4 w[NW][CT];
+        typename Group::scales s[NW][CT];
+        typename Group::zeros z[ZEROS ? NW : 1][ZEROS ? CT : 1];
+        bf16x8 x[NB][4];
+    };
+    auto load = [&](Batch &b, int kt) __attribute__((always_inline)) {
+        kt = min(kt, ktiles - 1); // past the end: loaded, not used
+#pragma unroll
+        for (int w = 0; w < NW; ++w)
+#pragma unroll
+            for (int c = 0; c < CT; ++c) {
+                const size_t at = tile[c] + kt;
+                b.w[w][c] = __builtin_nontemporal_load((const u32x4 *)(p.tiles[w] + at * 1024 + lane * 16));
+                b.s[w][c] = ((const typename Group::scales *)p.scales[w])[at * 16 + row];
+                if constexpr (ZEROS)
+                    b.z[w][c] = ((const typename Group::zeros *)p.zeros[w])[at * 16 + row];
+            }
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int k = kt * 128 + 32 * j; // rows past K multiply zeros
+                const uint32_t off = k + 8 * kq < K ? x_off[nb] + (uint32_t)k * 2u : kOutOfRange;
+                b.x[nb][j] = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(rx, off, 0, 0));
+            }
+    };
+    float total[NW][CT][NB][NR] = {};
+    const auto constant = [](uint32_t v) __attribute__((always_inline)) {
+        return __builtin_bit_cast(bf16x8, u32x4{v, v, v, v});
+    };
+    auto use = [&](const Batch &b) __attribute__((always_inline)) {
+#pragma unroll
+        for (int g = 0; g < GPT; ++g) {
+            f32x4 mid[NB];
+            if constexpr (!ZEROS)
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb) {
+                    mid[nb] = f32x4{};
+#pragma unroll
+                    for (int m = 0; m < MPG; ++m)
+                        mid[nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b.x[nb][g * MPG + m], constant(kW4MinusMid),
+                                                                          mid[nb], 0, 0, 0);
+                }
+#pragma unroll
+            for (int w = 0; w < NW; ++w)
+#pragma unroll
+                for (int c = 0; c < CT; ++c) {
+                    bf16x8 q[MPG];
+#pragma unroll
+                    for (int m = 0; m < MPG; ++m)
+                        q[m] = w4_unpack(b.w[w][c][g * MPG + m]);
+                    const float s = __builtin_bit_cast(float, Group::scale(b.s[w][c], g));
+#pragma unroll
+                    for (int nb = 0; nb < NB; ++nb) {
+                        f32x4 acc;
+                        if constexpr (ZEROS) {
+                            const uint32_t z = 0xbf80u | Group::zero(b.z[w][c], g); // -(1 + z / 128)
+                            acc = f32x4{};
+#pragma unroll
+                            for (int m = 0; m < MPG; ++m)
+                                acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b.x[nb][g * MPG + m], constant(z | z << 16),
+                                                                              acc, 0, 0, 0);
+                        } else {
+                            acc = mid[nb];
+                        }
+#pragma unroll
+                        for (int m = 0; m < MPG; ++m)
+                            acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b.x[nb][g * MPG + m], q[m], acc, 0, 0, 0);
+#pragma unroll
+                        for (int i = 0; i < NR; ++i)
+                            total[w][c][nb][i] += s * acc[i];
+                    }
+                }
+        }
+    };
+
+    Batch batch[DEPTH];
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d)
+        load(batch[d], begin + d);
+    int kt = begin;
+    for (; kt + DEPTH <= end; kt += DEPTH)
+#pragma unroll
+        for (int d = 0; d < DEPTH; ++d) {
+            use(batch[d]);
+            load(batch[d], kt + d + DEPTH);
+        }
+#pragma unroll
+    for (int d = 0; d < DEPTH; ++d)
+        if (kt + d < end)
+            use(batch[d]);
+
+    // ---- sums of the waves, in order ---------------------------------------------
+#pragma unroll
+    for (int w = 0; w < NW; ++w)
+#pragma unroll
+        for (int c = 0; c < CT; ++c)
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                for (int i = 0; i < NR; ++i)
+                    part[(wave * SLOTS + ((w * CT + c) * NB + nb) * NR + i) * 64 + lane] = total[w][c][nb][i];
+    __syncthreads();
+    constexpr int OUT = CT * NB * NR; // result slots of one weight
+    for (int slot = wave; slot < OUT; slot += WAVES) {
+        float v[NW];
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            v[w] = part[(w * OUT + slot) * 64 + lane];
+#pragma unroll
+            for (int o = 1; o < WAVES; ++o)
+                v[w] += part[(o * SLOTS + w * OUT + slot) * 64 + lane];
+            v[w] *= 128.0f; // the weights were (q - z) / 128
+        }
+        const int i = slot % NR, nb = slot / NR % NB, c = slot / (NR * NB);
+        const int t = 16 * nb + kq + 4 * i, n = (first + c) * 16 + row;
+        if (t < p.T && n < p.N) {
+            const float y = NW == 2 ? gate_act(v[0], p.activation, p.beta) * v[NW - 1] : v[0];
+            p.out[(size_t)t * p.N + n] = __builtin_bit_cast(uint16_t, (__bf16)y);
+        }
+    }
+}
+
+// ---- laying out, rounding and restoring weights -----------------------------------
+
+struct W4LayoutParams {
+    uint8_t *tiles, *scales, *zeros; // packed
+    uint8_t *q, *z;                  // [K, N], [groups, N]
+    uint16_t *s, *w;                 // [groups, N], [K, N]
+    int K, N, group, ktiles, ntiles;
+};
+
+// Thread i of the layout kernels: lane i % 64 of tile i / 64.
+__global__ __launch_bounds__(256) void w4_pack_kernel(W4LayoutParams p)
+{
+    const size_t id = (size_t)blockIdx.x * 256 + threadIdx.x;
+    const size_t tile = id >> 6;
+    if (tile >= (size_t)p.ktiles * p.ntiles)
+        return;
+    const int lane = id & 63, kt = tile % p.ktiles, n = (int)(tile / p.ktiles) * 16 + (lane & 15);
+    u32x4 out{};
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        uint32_t d = 0;
+        for (int e = 0; e < 8; ++e) {
+            const int k = kt * 128 + 32 * j + 8 * (lane >> 4) + e;
+            if (k < p.K && n < p.N)
+                d |= (uint32_t)(p.q[(size_t)k * p.N + n] & 15) << (4 * (e >> 1) + 16 * (e & 1));
+        }
+        out[j] = d;
+    }
+    *(u32x4 *)(p.tiles + id * 16) = out;
+    if (lane < 16) {
+        const int gpt = 128 / p.group, groups = (p.K + p.group - 1) / p.group;
+        for (int g = 0; g < gpt; ++g) {
+            const int at = kt * gpt + g;
+            const bool in = at < groups && n < p.N;
+            const size_t to = (tile * 16 + lane) * gpt + g;
+            ((uint16_t *)p.scales)[to] = in ? p.s[(size_t)at * p.N + n] : 0;
+            if (p.zeros)
+                p.zeros[to] = in ? p.z[(size_t)at * p.N + n] & 15 : 0;
+        }
+    }
+}
+
+__global__ __launch_bounds__(256) void w4_dequantize_kernel(W4LayoutParams p)
+{
+    const size_t id = (size_t)blockIdx.x * 256 + threadIdx.x;
+    const size_t tile = id >> 6;
+    if (tile >= (size_t)p.ktiles * p.ntiles)
+        return;
+    const int lane = id & 63, kt = tile % p.ktiles, n = (int)(tile / p.ktiles) * 16 + (lane & 15);
+    if (n >= p.N)
+        return;
+    const u32x4 in = *(const u32x4 *)(p.tiles + id * 16);
+    const int gpt = 128 / p.group;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+        const size_t at = (tile * 16 + (lane & 15)) * gpt + 32 * j / p.group;
+        const uint32_t sb = ((const uint16_t *)p.scales)[at];
+        const float s = __builtin_bit_cast(float, sb << 16);
+        const int z = p.zeros ? p.zeros[at] : 8;
+        for (int e = 0; e < 8; ++e) {
+            const int k = kt * 128 + 32 * j + 8 * (lane >> 4) + e;
+            const int q = in[j] >> (4 * (e >> 1) + 16 * (e & 1)) & 15;
+            if (k < p.K)
+                p.w[(size_t)k * p.N + n] = __builtin_bit_cast(uint16_t, (__bf16)((float)(q - z) * s));
+        }
+    }
+}
+
+// One thread per column and group; the groups' blocks follow one another.
+__global__ __launch_bounds__(256) void w4_quantize_kernel(W4LayoutParams p)
+{
+    const int columns = (p.N + 255) / 256, g = blockIdx.x / columns;
+    const int n = (blockIdx.x % columns) * 256 + threadIdx.x;
+    if (n >= p.N)
+        return;
+    const int first = g * p.group, last = min(p.K, first + p.group);
+    float lo = 0.0f, hi = 0.0f;
+    for (int k = first; k < last; ++k) {
+        const float w = __builtin_bit_cast(float, (uint32_t)p.w[(size_t)k * p.N + n] << 16);
+        lo = fminf(lo, w);
+        hi = fmaxf(hi, w);
+    }
+    const float range = p.z ? (hi - lo) / 15.0f : fmaxf(-lo, hi) / 7.0f;
+    const uint16_t bits = __builtin_bit_cast(uint16_t, (__bf16)range);
+    const float s = __builtin_bit_cast(float, (uint32_t)bits << 16);
+    const float z = !p.z ? 8.0f : s > 0.0f ? fminf(rintf(-lo / s), 15.0f) : 0.0f;
+    for (int k = first; k < last; ++k) {
+        const float w = __builtin_bit_cast(float, (uint32_t)p.w[(size_t)k * p.N + n] << 16);
+        const float q = s > 0.0f ? fminf(fmaxf(rintf(w / s) + z, 0.0f), 15.0f) : z;
+        p.q[(size_t)k * p.N + n] = (uint8_t)q;
+    }
+    p.s[(size_t)g * p.N + n] = bits;
+    if (p.z)
+        p.z[(size_t)g * p.N + n] = (uint8_t)z;
+}
+
+} // namespace gmlp

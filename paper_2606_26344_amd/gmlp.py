@@ -34,7 +34,7 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIBRARY = os.path.join(HERE, "libgmlp.so")
 HEADER = os.path.join(os.path.dirname(HERE), "include", "gmlp.h")
 HEADERS = [os.path.join(os.path.dirname(HERE), "include", h)
-           for h in ("gmlp.h", "softmax_matmul.h", "gmlp_train.h", "gmlp_block_norm.h")]
+           for h in ("gmlp.h", "softmax_matmul.h", "gmlp_train.h", "gmlp_block_norm.h", "gmlp_w4.h")]
 
 PATH_AUTO, PATH_GEMV, PATH_MFMA, PATH_FUSED, PATH_FUSED_MFMA = 0, 1, 2, 3, 4
 _PATHS = {"auto": PATH_AUTO, "gemv": PATH_GEMV, "mfma": PATH_MFMA, "fused": PATH_FUSED,
@@ -87,6 +87,14 @@ _SIGNATURES = {
     "gmlp_block_norm": ([_P] * 7 + [_I64, _I64, _INT, _F, _F, _P], _INT),
     "gmlp_block_norm_workspace_size": ([_I64, _I64], _SZ),
     "gmlp_block_norm_backward": ([_P] * 12 + [_I64, _I64, _INT, _F, _F, _P, _SZ, _P], _INT),
+    "gmlp_w4_packed_size": ([_I64, _I64, _INT, _INT], _SZ),
+    "gmlp_w4_quantize": ([_P] * 4 + [_I64, _I64, _INT, _P], _INT),
+    "gmlp_w4_pack": ([_P] * 4 + [_I64, _I64, _INT, _P], _INT),
+    "gmlp_w4_dequantize": ([_P] * 2 + [_I64, _I64, _INT, _INT, _P], _INT),
+    "gmlp_w4_workspace_size": ([_I64, _I64, _I64], _SZ),
+    "gmlp_w4_matmul": ([_P] * 3 + [_I64, _I64, _I64, _INT, _INT, _INT, _P, _SZ, _P], _INT),
+    "gmlp_w4_gate_up": ([_P] * 4 + [_I64, _I64, _I64, _INT, _INT, _INT, _F, _INT, _P, _SZ, _P], _INT),
+    "gmlp_w4_forward": ([_P] * 5 + [_I64, _I64, _I64, _INT, _INT, _INT, _F, _INT, _P, _SZ, _P], _INT),
 }
 
 _lib = None
