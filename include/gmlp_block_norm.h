@@ -47,7 +47,7 @@
 extern "C" {
 #endif
 
-#define GMLP_NORM_MAX_WIDTH 32768
+#define GMLP_NORM_MAX_WIDTH 16384
 
 enum gmlp_norm_flags {
     GMLP_NORM_POST = 1,      /* the norm after the block */

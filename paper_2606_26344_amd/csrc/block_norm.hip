@@ -13,9 +13,32 @@ using namespace gmlp;
 
 namespace {
 
-constexpr int kNormForwardBlocks = 2048, kNormBackwardBlocks = 512;
+// Threads of a row, rows of a block and blocks of a launch.
+struct NormShape {
+    int chunks = 1; // 16-byte chunks per thread
+    int row_threads = 64, row_groups = 1, blocks = 1;
+    int threads() const { return row_threads * row_groups; }
+};
 
-int norm_blocks(int64_t T, int most) { return (int)std::min<int64_t>(std::max<int64_t>(T, 1), most); }
+// One chunk per thread up to 8192 columns, then 2.  As many rows in a block
+// as `threads` hold, but first a block for each of the 256 CUs; at most
+// `most_blocks` blocks, which then take several rows in turn.
+NormShape norm_shape(int64_t T, int64_t D, int threads, int most_blocks)
+{
+    NormShape s;
+    const int64_t chunks = D / 8;
+    s.chunks = chunks <= kNormMaxThreads ? 1 : 2;
+    s.row_threads = (int)cdiv(cdiv(chunks, s.chunks), 64) * 64;
+    T = std::max<int64_t>(T, 1);
+    s.row_groups = (int)std::max<int64_t>(1, std::min<int64_t>(threads / s.row_threads, T / kBlockTarget));
+    s.blocks = (int)std::min<int64_t>(cdiv(T, s.row_groups), most_blocks);
+    return s;
+}
+
+// Forward: blocks of up to 512 threads, 4 for each CU.  Backward: one block of up
+// to 1024 threads for each CU, since every block adds a row of partial sums.
+NormShape norm_forward_shape(int64_t T, int64_t D) { return norm_shape(T, D, 512, 4 * kBlockTarget); }
+NormShape norm_backward_shape(int64_t T, int64_t D) { return norm_shape(T, D, kNormMaxThreads, kBlockTarget); }
 
 int check_norm_shape(int64_t T, int64_t D)
 {
@@ -71,31 +94,20 @@ int check_norm_spans(const NormSpan *in, int n_in, const NormSpan *out, int n_ou
     return GMLP_OK;
 }
 
-// f(threads, chunks) as integral constants for a row of D elements.
+// f(chunks) as an integral constant.
 template <class F>
-int with_norm_shape(int64_t D, F f)
+int with_norm_chunks(const NormShape &s, F f)
 {
     using std::integral_constant;
-    const int64_t chunks = D / 8;
-    if (chunks <= 64)
-        return f(integral_constant<int, 64>{}, integral_constant<int, 1>{});
-    if (chunks <= 128)
-        return f(integral_constant<int, 64>{}, integral_constant<int, 2>{});
-    if (chunks <= 256)
-        return f(integral_constant<int, 128>{}, integral_constant<int, 2>{});
-    if (chunks <= 512)
-        return f(integral_constant<int, 256>{}, integral_constant<int, 2>{});
-    if (chunks <= 1024)
-        return f(integral_constant<int, 512>{}, integral_constant<int, 2>{});
-    if (chunks <= 2048)
-        return f(integral_constant<int, 1024>{}, integral_constant<int, 2>{});
-    return f(integral_constant<int, 1024>{}, integral_constant<int, 4>{});
+    return s.chunks == 1 ? f(integral_constant<int, 1>{}) : f(integral_constant<int, 2>{});
 }
 
 NormParams norm_params(const void *y, const void *res, const void *w_pre, const void *w_post, const void *gate,
-                       int64_t T, int64_t D, int flags, float res_scale, float eps)
+                       int64_t T, int64_t D, int flags, float res_scale, float eps, const NormShape &shape)
 {
     NormParams p{};
+    p.row_threads = shape.row_threads;
+    p.row_groups = shape.row_groups;
     p.y = static_cast<const uint16_t *>(y);
     p.res = res;
     p.w_pre = static_cast<const uint16_t *>(w_pre);
@@ -134,17 +146,18 @@ int gmlp_block_norm(const void *Y, const void *res, const void *w_pre, const voi
     const NormSpan out[] = {{R, b * e, "R", res}, {Xn, 2 * e, "Xn", Y}};
     if ((rc = check_norm_spans(in, 5, out, 2, nullptr, 0)))
         return rc;
-    NormParams p = norm_params(Y, res, w_pre, w_post, gate, T, D, flags, res_scale, eps);
+    const NormShape shape = norm_forward_shape(T, D);
+    NormParams p = norm_params(Y, res, w_pre, w_post, gate, T, D, flags, res_scale, eps, shape);
     p.r_out = R;
     p.xn = static_cast<uint16_t *>(Xn);
     hipStream_t st = static_cast<hipStream_t>(stream);
-    rc = with_norm_shape(D, [&](auto threads, auto chunks) {
-        constexpr int NT = decltype(threads)::value, CH = decltype(chunks)::value;
-        const dim3 grid(norm_blocks(T, kNormForwardBlocks)), block(NT);
+    rc = with_norm_chunks(shape, [&](auto chunks) {
+        constexpr int CH = decltype(chunks)::value;
+        const dim3 grid(shape.blocks), block(shape.threads());
         if (flags & GMLP_NORM_RES_FP32)
-            hipLaunchKernelGGL((norm_forward_kernel<NT, CH, true>), grid, block, 0, st, p);
+            hipLaunchKernelGGL((norm_forward_kernel<CH, true>), grid, block, 0, st, p);
         else
-            hipLaunchKernelGGL((norm_forward_kernel<NT, CH, false>), grid, block, 0, st, p);
+            hipLaunchKernelGGL((norm_forward_kernel<CH, false>), grid, block, 0, st, p);
         return hip_check(hipGetLastError(), "norm launch");
     });
     return rc ? rc : ok();
@@ -154,7 +167,7 @@ size_t gmlp_block_norm_workspace_size(int64_t T, int64_t D)
 {
     if (check_norm_shape(T, D))
         return 0;
-    return align_up((size_t)3 * norm_blocks(T, kNormBackwardBlocks) * D * sizeof(float));
+    return align_up((size_t)kNormSums * norm_backward_shape(T, D).blocks * D * sizeof(float));
 }
 
 int gmlp_block_norm_backward(const void *dXn, const void *dR, const void *Y, const void *R, const void *w_pre,
@@ -180,7 +193,7 @@ int gmlp_block_norm_backward(const void *dXn, const void *dR, const void *Y, con
         return fail(GMLP_ERR_INVALID_ARG, "dgate without a gate");
     if (rows && dY && !Y)
         return fail(GMLP_ERR_INVALID_ARG, "dY without Y");
-    const int sums = (dw_pre ? 1 : 0) | (dw_post ? 2 : 0) | (dgate && !gate_rows ? 4 : 0);
+    const int sums = (dw_pre ? 1 : 0) | (dw_post || (dgate && !gate_rows) ? 2 : 0);
     const size_t need = gmlp_block_norm_workspace_size(T, D);
     if (sums) {
         if (!workspace)
@@ -199,10 +212,10 @@ int gmlp_block_norm_backward(const void *dXn, const void *dR, const void *Y, con
     if ((rc = check_norm_spans(in, 7, out, 5, sums ? workspace : nullptr, need)))
         return rc;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    const int blocks = norm_blocks(T, kNormBackwardBlocks);
+    const NormShape shape = norm_backward_shape(T, D);
     float *partial = static_cast<float *>(workspace);
     if (rows && (dY || dres || sums || dgate)) {
-        NormParams p = norm_params(Y, R, w_pre, w_post, gate, T, D, flags, res_scale, eps);
+        NormParams p = norm_params(Y, R, w_pre, w_post, gate, T, D, flags, res_scale, eps, shape);
         p.dxn = static_cast<const uint16_t *>(dXn);
         p.dr = dR;
         p.dy = static_cast<uint16_t *>(dY);
@@ -210,22 +223,30 @@ int gmlp_block_norm_backward(const void *dXn, const void *dR, const void *Y, con
         p.dgate = gate_rows ? static_cast<uint16_t *>(dgate) : nullptr;
         p.partial = partial;
         p.sums = sums;
-        rc = with_norm_shape(D, [&](auto threads, auto chunks) {
-            constexpr int NT = decltype(threads)::value, CH = decltype(chunks)::value;
+        rc = with_norm_chunks(shape, [&](auto chunks) {
+            constexpr int CH = decltype(chunks)::value;
+            const dim3 grid(shape.blocks), block(shape.threads());
             if (flags & GMLP_NORM_RES_FP32)
-                hipLaunchKernelGGL((norm_backward_kernel<NT, CH, true>), dim3(blocks), dim3(NT), 0, st, p);
+                hipLaunchKernelGGL((norm_backward_kernel<CH, true>), grid, block, 0, st, p);
             else
-                hipLaunchKernelGGL((norm_backward_kernel<NT, CH, false>), dim3(blocks), dim3(NT), 0, st, p);
+                hipLaunchKernelGGL((norm_backward_kernel<CH, false>), grid, block, 0, st, p);
             return hip_check(hipGetLastError(), "norm backward launch");
         });
         if (rc)
             return rc;
     }
     if (sums) {
-        hipLaunchKernelGGL(norm_columns_kernel, dim3((unsigned)cdiv(D, kNormColumns), 3),
-                           dim3(kNormColumns * kNormGroups), 0, st, partial, static_cast<uint16_t *>(dw_pre),
-                           static_cast<uint16_t *>(dw_post), sums & 4 ? static_cast<uint16_t *>(dgate) : nullptr,
-                           rows ? blocks : 0, (int)D);
+        NormColumns c{};
+        c.partial = partial;
+        c.w_post = static_cast<const uint16_t *>(w_post);
+        c.gate = gate_rows ? nullptr : static_cast<const uint16_t *>(gate);
+        c.dw_pre = static_cast<uint16_t *>(dw_pre);
+        c.dw_post = static_cast<uint16_t *>(dw_post);
+        c.dgate = gate_rows ? nullptr : static_cast<uint16_t *>(dgate);
+        c.blocks = rows ? shape.blocks : 0;
+        c.D = (int)D;
+        hipLaunchKernelGGL(norm_columns_kernel, dim3((unsigned)cdiv(D, kNormColumns), kNormSums),
+                           dim3(kNormColumns * kNormGroups), 0, st, c);
         if ((rc = hip_check(hipGetLastError(), "norm column sums launch")))
             return rc;
     }

@@ -117,6 +117,26 @@ struct AccBlock<true> {
     __device__ static int tok(int j, int lane) { return 16 * (j >> 1) + (lane & 15); }
 };
 
+// The accumulators of 16 rows x 32 columns, two 16 x 16 MFMA results, as eight
+// neighbouring columns per lane: the 16-lane groups 0, 1, 2, 3 hold columns 4 g .. of
+// either, and swapping the odd groups of the first with the even ones of the second
+// leaves columns 0 .., 16 .., 8 .., 24 .. in them.  Outputs are then 16 bytes per
+// lane and 64 per row; stores of 8 and 32 bytes held the weight gradients of few
+// tokens to 2.5 TB/s.
+__device__ __forceinline__ void wide_columns(const f32x4 &lo, const f32x4 &hi, float (&v)[8])
+{
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const float a = lo[e], b = hi[e];
+        const auto r = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b),
+                                                        false, false);
+        const uint32_t x = r[0], y = r[1];
+        v[e] = __builtin_bit_cast(float, x);
+        v[4 + e] = __builtin_bit_cast(float, y);
+    }
+}
+__device__ __forceinline__ int wide_column(int lane) { return 16 * (lane >> 4 & 1) + 8 * (lane >> 5); }
+
 // Physical chunk of logical chunk c in LDS row r of an activation tile
 // (rows of 8 chunks): any 8, and any aligned 16, consecutive rows reading
 // one logical chunk hit distinct banks.
@@ -735,25 +755,60 @@ __device__ __forceinline__ int gemm_block(const GemmParams &p, int block, StageP
     const bool scaled = EPI == EPI_GATE_MUL && p.rrms;
     const bool divided = EPI == EPI_STORE && p.rowdiv;
     if constexpr (EPI == EPI_GATE_SAVE) {
-        // G and U, each rounded once; H below takes the unrounded values.
-        const __amdgpu_buffer_rsrc_t rg = make_rsrc(p.out_g + (size_t)n0 * M + m0);
-        const __amdgpu_buffer_rsrc_t ru = make_rsrc(p.out_u + (size_t)n0 * M + m0);
+        // G, U and H, each rounded once (H from the unrounded G and U); with 16x16
+        // subtiles as eight columns per lane.
+        const auto at = [&](const uint16_t *t) { return make_rsrc(t + (size_t)n0 * M + m0); };
+        const __amdgpu_buffer_rsrc_t rg = at(p.out_g), ru = at(p.out_u), rh = at(p.out);
+        const auto in_range = [&](int tl, int fl) {
+            const int in = (int)(n0 + tl < N) & (int)(m0 + fl < M); // without a branch
+            return in ? ((uint32_t)tl * (uint32_t)M + (uint32_t)fl) * 2u : kOutOfRange;
+        };
 #pragma unroll
-        for (int mi = 0; mi < TM; ++mi)
+        for (int ni = 0; ni < TN; ++ni)
 #pragma unroll
-            for (int ni = 0; ni < TN; ++ni)
+            for (int mi = 0; mi < TM; ++mi) {
+                if constexpr (M16) {
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int fl = wm * TM * 32 + mi * 32 + A::col(j, lane);
-                    const int tl = wn * TN * 32 + ni * 32 + A::tok(j, lane);
-                    const uint32_t off = n0 + tl < N && m0 + fl < M ? (uint32_t)(tl * M + fl) * 2u : kOutOfRange;
-                    const f32x4 g = acc[0][mi][ni].piece(j), u = acc[NW - 1][mi][ni].piece(j);
-                    __builtin_amdgcn_raw_buffer_store_b64(u32x2{pack_bf16x2(g[0], g[1]), pack_bf16x2(g[2], g[3])}, rg,
-                                                          off, 0, OUT_POLICY);
-                    __builtin_amdgcn_raw_buffer_store_b64(u32x2{pack_bf16x2(u[0], u[1]), pack_bf16x2(u[2], u[3])}, ru,
-                                                          off, 0, OUT_POLICY);
-                    __builtin_amdgcn_sched_barrier(0);
+                    for (int h = 0; h < 2; ++h) {
+                        float g[8], u[8];
+                        wide_columns(acc[0][mi][ni].v[2 * h], acc[0][mi][ni].v[2 * h + 1], g);
+                        wide_columns(acc[NW - 1][mi][ni].v[2 * h], acc[NW - 1][mi][ni].v[2 * h + 1], u);
+                        const uint32_t off = in_range(wn * TN * 32 + ni * 32 + 16 * h + (lane & 15),
+                                                      wm * TM * 32 + mi * 32 + wide_column(lane));
+                        u32x4 pg, pu, ph;
+#pragma unroll
+                        for (int q = 0; q < 4; ++q) {
+                            pg[q] = pack_bf16x2(g[2 * q], g[2 * q + 1]);
+                            pu[q] = pack_bf16x2(u[2 * q], u[2 * q + 1]);
+                            ph[q] = pack_bf16x2(gate_act(g[2 * q], p.activation, p.beta) * u[2 * q],
+                                                gate_act(g[2 * q + 1], p.activation, p.beta) * u[2 * q + 1]);
+                        }
+                        __builtin_amdgcn_raw_buffer_store_b128(pg, rg, off, 0, OUT_POLICY);
+                        __builtin_amdgcn_raw_buffer_store_b128(pu, ru, off, 0, OUT_POLICY);
+                        __builtin_amdgcn_raw_buffer_store_b128(ph, rh, off, 0, OUT_POLICY);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const uint32_t off = in_range(wn * TN * 32 + ni * 32 + A::tok(j, lane),
+                                                      wm * TM * 32 + mi * 32 + A::col(j, lane));
+                        const f32x4 g = acc[0][mi][ni].piece(j), u = acc[NW - 1][mi][ni].piece(j);
+                        float h[4];
+#pragma unroll
+                        for (int e = 0; e < 4; ++e)
+                            h[e] = gate_act(g[e], p.activation, p.beta) * u[e];
+                        __builtin_amdgcn_raw_buffer_store_b64(u32x2{pack_bf16x2(g[0], g[1]), pack_bf16x2(g[2], g[3])},
+                                                              rg, off, 0, OUT_POLICY);
+                        __builtin_amdgcn_raw_buffer_store_b64(u32x2{pack_bf16x2(u[0], u[1]), pack_bf16x2(u[2], u[3])},
+                                                              ru, off, 0, OUT_POLICY);
+                        __builtin_amdgcn_raw_buffer_store_b64(u32x2{pack_bf16x2(h[0], h[1]), pack_bf16x2(h[2], h[3])},
+                                                              rh, off, 0, OUT_POLICY);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }
                 }
+            }
+        return m0;
     }
     // All of the wave's packed results first, each group of 4 columns into
     // registers of its own, then the stores back to back: a store's data
@@ -770,7 +825,7 @@ __device__ __forceinline__ int gemm_block(const GemmParams &p, int block, StageP
                 float v[4];
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    if constexpr (EPI == EPI_GATE_MUL || EPI == EPI_GATE_SAVE) {
+                    if constexpr (EPI == EPI_GATE_MUL) {
                         float g = acc[0][mi][ni].get(4 * j + e), u = acc[NW - 1][mi][ni].get(4 * j + e);
                         if (scaled) {
                             g *= rs[ni][h];

@@ -8,104 +8,182 @@
 namespace gmlp {
 
 // A tile configuration of the gradient matmuls (gemm_grad.hpp): a WM x WN grid
-// of waves, each holding TM x TN blocks of 32 x 32 outputs, STAGES LDS stages of
-// 64 contracted elements.  "m" counts output columns, "n" output rows.
-template <int WM_, int WN_, int TM_, int TN_, int STAGES_>
+// of waves, each holding TM x TN blocks of 32 x 32 outputs, STAGES LDS stages of BK
+// contracted elements, BLOCKS blocks on a CU.  "m" counts output columns, "n" output
+// rows.
+template <int WM_, int WN_, int TM_, int TN_, int STAGES_, int BK_, int BLOCKS_>
 struct GradShape {
-    static constexpr int WM = WM_, WN = WN_, TM = TM_, TN = TN_, STAGES = STAGES_;
-    static constexpr int BK = 64;
+    static constexpr int WM = WM_, WN = WN_, TM = TM_, TN = TN_, STAGES = STAGES_, BK = BK_, BLOCKS = BLOCKS_;
     static constexpr int NWAVES = WM * WN, NTHREADS = 64 * NWAVES;
     static constexpr int BM = WM * TM * 32, BN = WN * TN * 32;
     static constexpr int A_BYTES = BM * BK * 2, B_BYTES = BN * BK * 2;
     static constexpr int STAGE_BYTES = A_BYTES + B_BYTES;
     static constexpr int LOADS_PER_STAGE = STAGE_BYTES / (NTHREADS * 16);
     static constexpr int PIECES = TM * TN * 4; // 16-byte pieces of accumulators per lane
-    static_assert(BM % 128 == 0 && BN % 128 == 0, "transposing reads of 128- or 256-element rows");
+    static_assert(BK == 32 || BK == 64, "k-tile of 32 or 64");
+    static_assert(BM % 128 == 0, "transposing reads of 128- or 256-element rows");
     static_assert(A_BYTES % (NTHREADS * 16) == 0 && B_BYTES % (NTHREADS * 16) == 0, "whole 16-byte loads");
     static_assert(STAGES >= 2 && STAGES <= 4, "2..4 LDS stages");
-    static_assert(STAGES * STAGE_BYTES + 64 <= 160 * 1024, "LDS capacity of a CU");
+    static_assert(BLOCKS * (STAGES * STAGE_BYTES + 1024) <= 160 * 1024, "LDS capacity of a CU");
     static_assert((STAGES - 2) * LOADS_PER_STAGE < 64, "vmcnt range");
 };
 
 namespace {
 
-using GradLarge = GradShape<4, 2, 2, 4, 2>; // 256 x 256, 8 waves
-using GradSmall = GradShape<2, 2, 2, 2, 4>; // 128 x 128, 4 waves
+// Tiles of the gradient matmuls.  The tall ones are for the products with a
+// weight (dH, dX) of few tokens: 128 rows of the weight against all the tokens, so
+// that each weight element is staged once.  The pair is for weight gradients of few
+// tokens: the stores and first loads of one block go on beside the MFMAs of the
+// other.  Measured, us, dH and dX for each tile and dW (D = 4096, F = 14336; in
+// brackets D = 5120, F = 13824):
+//   dH + dX  T = 16    128 x 32 83, 64 86, 128 89, 192 96, 320 111, 256 x 256 112
+//            T = 64    128 x 64 95, 32 108 (dX), 128 100, 256 x 256 147 (dX)
+//            T = 300   [dX: 128 x 160 104, 320 107, 128 107, 256 x 256 129]
+//   dW       T = 16    256 x 256 103, pair 90, 128 x 128 158
+//            T = 300   [200, 173, 284]
+//            T = 600   263, 244, 344
+//            T = 4096  1100, 1190, 1500
+using GradLarge = GradShape<4, 2, 2, 4, 2, 64, 1>;   // 256 x 256, 8 waves
+using GradPair = GradShape<2, 2, 2, 4, 2, 32, 2>;    // 128 x 256, 4 waves, two blocks on a CU
+using GradSmall = GradShape<2, 2, 2, 2, 4, 64, 1>;   // 128 x 128, 4 waves
+using GradTall32 = GradShape<4, 1, 1, 1, 4, 64, 1>;  // 128 x 32, 4 waves
+using GradTall64 = GradShape<4, 1, 1, 2, 4, 64, 1>;  // 128 x 64, 4 waves
+using GradTall96 = GradShape<4, 1, 1, 3, 4, 64, 1>;  // 128 x 96, 4 waves
+using GradTall160 = GradShape<4, 1, 1, 5, 4, 64, 1>; // 128 x 160, 4 waves
+using GradTall192 = GradShape<4, 1, 1, 6, 3, 64, 1>; // 128 x 192, 4 waves
+using GradTall320 = GradShape<4, 2, 1, 5, 2, 64, 1>; // 128 x 320, 8 waves
+enum GradTile { GRAD_LARGE, GRAD_SMALL, GRAD_PAIR, GRAD_T32, GRAD_T64, GRAD_T96, GRAD_T160, GRAD_T192, GRAD_T320, GRAD_TILES };
 
-// One matmul launch of the backward pass.
+template <class S, GradTile T>
+struct GradShapeTag {
+    using type = S;
+    static constexpr GradTile tile = T;
+};
+// f(GradShapeTag<shape, tile>) of a tile.
+template <class F>
+auto with_grad_tile(GradTile t, F f)
+{
+    switch (t) {
+    case GRAD_LARGE: return f(GradShapeTag<GradLarge, GRAD_LARGE>{});
+    case GRAD_PAIR: return f(GradShapeTag<GradPair, GRAD_PAIR>{});
+    case GRAD_T32: return f(GradShapeTag<GradTall32, GRAD_T32>{});
+    case GRAD_T64: return f(GradShapeTag<GradTall64, GRAD_T64>{});
+    case GRAD_T96: return f(GradShapeTag<GradTall96, GRAD_T96>{});
+    case GRAD_T160: return f(GradShapeTag<GradTall160, GRAD_T160>{});
+    case GRAD_T192: return f(GradShapeTag<GradTall192, GRAD_T192>{});
+    case GRAD_T320: return f(GradShapeTag<GradTall320, GRAD_T320>{});
+    default: return f(GradShapeTag<GradSmall, GRAD_SMALL>{});
+    }
+}
+
+// One matmul launch of the backward pass: whole tiles, and the rest in `splits`
+// pieces of kt_split k-tiles each.
 struct GradStep {
-    bool large = false;
-    int tiles = 0;      // of all its problems
-    int nk = 0;         // k-tiles, of all segments
-    int kt_split = 0;   // k-tiles per split
-    int splits = 1;
-    int blocks = 0;
+    GradTile tile = GRAD_SMALL;
+    int nk = 0; // k-tiles of a tile, of all segments
+    int kt_seg = 0;
+    int64_t tiles = 0; // of all its problems
+    int64_t whole = 0;
+    int rest = 0, splits = 1, kt_split = 0;
+    int64_t blocks = 0;
+    int threads = 0;
     int counters = 0;
     size_t partial_bytes = 0;
 };
 
-// Estimated time (us) of `tiles` tiles in `splits` splits of `ktiles` k-tiles on
-// one tile shape: rounds of one block per CU, a k-tile at the rate of its MFMAs
-// or its staged bytes, and the exchange as in split_time.
+// Time (us) of one k-tile on a CU that runs BLOCKS of them: its MFMAs, or its
+// operands on their way to LDS (50 to 55 GB/s for each CU).
 template <class S>
-double grad_time(int64_t ktiles, int64_t splits, int64_t tiles)
+double grad_tile_time()
 {
-    const double rounds = (double)cdiv(tiles * splits, kBlockTarget);
-    const double per_tile = std::max((double)S::BM * S::BN * S::BK * 2 / 5.0e6, (double)S::STAGE_BYTES / 50e3);
-    double t = rounds * ((double)ktiles * per_tile + 2.0);
-    if (splits > 1) {
-        const double bytes = (double)S::BM * S::BN * sizeof(float);
-        t += 4.0 + (double)splits * bytes / 54e3 + (double)(splits * tiles) * bytes / 8e6;
-    }
-    return t;
+    return S::BLOCKS * std::max((double)S::BM * S::BN * S::BK * 2 / 5.4e6, (double)S::STAGE_BYTES / (S::BLOCKS > 1 ? 55e3 : 50e3));
 }
 
+// `problems` matmuls of M x N outputs (or N x M), `segments` contractions of K
+// each, on one tile, and the estimated time: whole rounds of tiles, the rest split
+// over k where that is faster, an exchange as in split_time, and at least the time
+// that the weights take from memory.
 template <class S>
-double grad_candidate(GradStep &s, bool large, int problems, int64_t M, int64_t N, int nk)
+double grad_candidate(GradStep &s, GradTile tile, int problems, int64_t M, int64_t N, int64_t K, int segments)
 {
-    s.large = large;
-    s.nk = nk;
-    const int64_t tiles = problems * cdiv(M, S::BM) * cdiv(N, S::BN);
-    s.tiles = (int)tiles;
-    double best = 0.0;
-    const int64_t most = tiles < kBlockTarget ? std::min<int64_t>(kBlockTarget / tiles, std::max(1, nk / 2)) : 1;
-    for (int64_t n = 1; n <= most; ++n) {
-        const int64_t per = cdiv(nk, n), splits = cdiv(nk, per);
-        const double t = grad_time<S>(per, splits, tiles);
-        if (n == 1 || t < best) {
-            best = t;
-            s.kt_split = (int)per;
-            s.splits = (int)splits;
+    s.tile = tile;
+    s.kt_seg = (int)std::max<int64_t>(1, cdiv(K, S::BK));
+    s.nk = segments * s.kt_seg;
+    s.threads = S::NTHREADS;
+    s.tiles = 0;
+    for (int i = 0; i < problems; ++i) // the third weight gradient is the transposed shape
+        s.tiles += std::max(cdiv(M, S::BM) * cdiv(N, S::BN), problems > 1 ? cdiv(N, S::BM) * cdiv(M, S::BN) : 0);
+    const int64_t round = (int64_t)S::BLOCKS * kBlockTarget;
+    s.whole = s.tiles / round * round;
+    s.rest = (int)(s.tiles - s.whole);
+    s.splits = 1;
+    s.kt_split = s.nk;
+    // A tile's first loads and its outputs, where no other block works beside it.
+    const double per = grad_tile_time<S>(), whole = s.nk * per + (S::BLOCKS > 1 ? 4.0 : 8.0);
+    double time = (double)(s.whole / round) * whole + 2.0;
+    if (s.rest) {
+        double best = whole;
+        const int64_t most = std::min<int64_t>(round / s.rest, std::max(1, s.nk / 2));
+        const double bytes = (double)S::BM * S::BN * sizeof(float);
+        for (int64_t n = 2; n <= most; ++n) {
+            const int64_t kt = cdiv(s.nk, n), splits = cdiv(s.nk, kt);
+            const double t = (double)kt * per + (whole - s.nk * per) + 4.0 + (double)splits * bytes / 54e3 + (double)(splits * s.rest) * bytes / 8e6;
+            if (t < best) {
+                best = t;
+                s.kt_split = (int)kt;
+                s.splits = (int)splits;
+            }
+        }
+        time += best;
+    }
+    s.blocks = s.whole + (int64_t)s.rest * s.splits;
+    s.counters = s.splits > 1 ? s.rest : 0;
+    s.partial_bytes = s.splits > 1 ? (size_t)s.rest * s.splits * S::BM * S::BN * sizeof(float) : 0;
+    // Every column of tiles reads the weight again, but from memory only once.
+    return std::max(time, (double)M * (double)K * segments * 2 / 5.0e6);
+}
+
+// Whether a launch may take a tile: weight gradients the pair, products with a
+// weight the tall ones.
+constexpr bool grad_tile_fits(GradTile t, bool weight)
+{
+    return t == GRAD_LARGE || t == GRAD_SMALL || (t == GRAD_PAIR) == weight;
+}
+
+// The tile with the least estimated time.
+inline GradStep grad_step(int problems, int64_t M, int64_t N, int64_t K, int segments, bool weight)
+{
+    GradStep best;
+    double best_time = 0.0;
+    for (int t = 0; t < GRAD_TILES; ++t) {
+        if (!grad_tile_fits((GradTile)t, weight))
+            continue;
+        GradStep s;
+        const double time = with_grad_tile((GradTile)t, [&](auto tag) {
+            return grad_candidate<typename decltype(tag)::type>(s, (GradTile)t, problems, M, N, K, segments);
+        });
+        if (t == 0 || time < best_time) {
+            best = s;
+            best_time = time;
         }
     }
-    s.blocks = s.tiles * s.splits;
-    s.counters = s.splits > 1 ? s.tiles : 0;
-    s.partial_bytes = s.splits > 1 ? (size_t)s.blocks * S::BM * S::BN * sizeof(float) : 0;
     return best;
 }
 
-// `problems` matmuls of M x N outputs (or N x M: the tiles are square), each
-// contracting nk k-tiles, on the shape with the smaller estimate.
-inline GradStep grad_step(int problems, int64_t M, int64_t N, int64_t nk)
-{
-    GradStep a, b;
-    const double ta = grad_candidate<GradLarge>(a, true, problems, M, N, (int)nk);
-    const double tb = grad_candidate<GradSmall>(b, false, problems, M, N, (int)nk);
-    return ta < tb ? a : b;
-}
-
 struct GradPlan {
-    GradStep dh, dx, dw;
+    GradStep dh, dx;
 };
 
 inline GradPlan grad_plan(int64_t T, int64_t D, int64_t F)
 {
     GradPlan p;
-    p.dh = grad_step(1, F, T, cdiv(D, 64));
-    p.dx = grad_step(1, D, T, 2 * cdiv(F, 64));
-    p.dw = grad_step(3, F, D, cdiv(T, 64));
+    p.dh = grad_step(1, F, T, D, 1, false);
+    p.dx = grad_step(1, D, T, F, 2, false);
     return p;
 }
+
+// The weight gradients, as many as are wanted.
+inline GradStep grad_weight_step(int problems, int64_t T, int64_t D, int64_t F) { return grad_step(problems, F, D, T, 1, true); }
 
 // The gate/up step of the training forward pass: the tiles of make_plan that
 // cover every token count, with H, G and U in the epilogue.
@@ -142,7 +220,7 @@ inline TrainLayout train_layout(int64_t T, int64_t D, int64_t F)
     size_t partial = std::max({s.partial_bytes, g.dh.partial_bytes, g.dx.partial_bytes});
     l.counters = std::max({l.fwd.counters, s.counters, g.dh.counters, g.dx.counters});
     for (int problems = 1; problems <= 3; ++problems) { // calls may want one, two or three of the weight gradients
-        const GradStep dw = grad_step(problems, F, D, cdiv(T, 64));
+        const GradStep dw = grad_weight_step(problems, T, D, F);
         partial = std::max(partial, dw.partial_bytes);
         l.counters = std::max(l.counters, dw.counters);
     }

@@ -47,8 +47,8 @@ int check_train_path(int path)
 // One launch of a GEMM kernel takes fewer than 2^32 threads.
 int check_grid(const GradStep &s)
 {
-    if ((int64_t)s.tiles * s.splits * (s.large ? GradLarge::NTHREADS : GradSmall::NTHREADS) >= (int64_t(1) << 32))
-        return fail(GMLP_ERR_UNSUPPORTED, "%d tiles exceed a launch grid", s.tiles);
+    if (s.blocks * s.threads >= (int64_t(1) << 32))
+        return fail(GMLP_ERR_UNSUPPORTED, "%lld tiles exceed a launch grid", (long long)s.tiles);
     return GMLP_OK;
 }
 
@@ -58,7 +58,7 @@ int check_train_shape(int64_t T, int64_t D, int64_t F)
     if ((rc = check_shape(T, D, F)))
         return rc;
     const GradPlan g = grad_plan(std::max<int64_t>(T, 1), D, F);
-    if ((rc = check_grid(g.dh)) || (rc = check_grid(g.dx)) || (rc = check_grid(g.dw)))
+    if ((rc = check_grid(g.dh)) || (rc = check_grid(g.dx)) || (rc = check_grid(grad_weight_step(3, T, D, F))))
         return rc;
     return GMLP_OK;
 }
@@ -100,26 +100,38 @@ int run_save(const Step &s, const void *X, const void *Wg, const void *Wu, void 
     }
 }
 
+// KC: a product with a weight; else a weight gradient.
 template <bool KC, int EPI, int SEGS>
 int launch_grad(const GradStep &s, GradParams p, const char *what, hipStream_t st)
 {
     p.nk = s.nk;
-    p.kt_split = s.kt_split;
+    p.kt_seg = s.kt_seg;
+    p.whole = (int)s.whole;
+    p.rest = s.rest;
     p.splits = s.splits;
-    p.tiles = s.tiles;
-    if (s.large)
-        hipLaunchKernelGGL((gemm_grad_kernel<GradLarge, KC, EPI, SEGS>), dim3(s.blocks), dim3(GradLarge::NTHREADS), 0, st, p);
-    else
-        hipLaunchKernelGGL((gemm_grad_kernel<GradSmall, KC, EPI, SEGS>), dim3(s.blocks), dim3(GradSmall::NTHREADS), 0, st, p);
-    return hip_check(hipGetLastError(), what);
+    p.kt_split = s.kt_split;
+    return with_grad_tile(s.tile, [&](auto tag) {
+        using S = typename decltype(tag)::type;
+        if constexpr (!grad_tile_fits(decltype(tag)::tile, !KC))
+            return fail(GMLP_ERR_INVALID_ARG, "internal: no kernel for this tile");
+        else {
+            hipLaunchKernelGGL((gemm_grad_kernel<S, KC, EPI, SEGS>), dim3((unsigned)s.blocks), dim3(S::NTHREADS), 0, st, p);
+            return hip_check(hipGetLastError(), what);
+        }
+    });
 }
 
 std::string grad_line(const GradStep &s, const char *args)
 {
+    const std::string shape = with_grad_tile(s.tile, [](auto tag) {
+        using S = typename decltype(tag)::type;
+        return std::to_string(S::WM) + ", " + std::to_string(S::WN) + ", " + std::to_string(S::TM) + ", " +
+               std::to_string(S::TN) + ", " + std::to_string(S::STAGES) + ", " + std::to_string(S::BK) + ", " +
+               std::to_string(S::BLOCKS);
+    });
     char tmp[160];
-    snprintf(tmp, sizeof tmp, "gemm_grad_kernel<GradShape<%s>, %s> grid=%d block=%d k_splits=%d\n",
-             s.large ? "4, 2, 2, 4, 2" : "2, 2, 2, 2, 4", args, s.blocks,
-             s.large ? GradLarge::NTHREADS : GradSmall::NTHREADS, s.splits);
+    snprintf(tmp, sizeof tmp, "gemm_grad_kernel<GradShape<%s>, %s> grid=%lld block=%d k_splits=%d\n", shape.c_str(), args,
+             (long long)s.blocks, s.threads, s.splits);
     return tmp;
 }
 
@@ -147,7 +159,7 @@ int gmlp_train_describe(int64_t T, int64_t D, int64_t F, int backward, char *buf
         const GradPlan g = grad_plan(std::max<int64_t>(T, 1), D, F);
         if (T > 0)
             text = grad_line(g.dh, "true, 1, 1") + grad_line(g.dx, "true, 0, 2");
-        text += grad_line(g.dw, "false, 0, 1");
+        text += grad_line(grad_weight_step(3, T, D, F), "false, 0, 1");
     } else if (T > 0) {
         const Step s = train_gate_up_step(T, D, F);
         text = describe_step(s, true);
@@ -228,7 +240,7 @@ int gmlp_train_backward(const void *dY, const void *X, const void *Wg, const voi
     uint16_t *H = reinterpret_cast<uint16_t *>(ws + l.fwd.h_off);
     uint16_t *dG = reinterpret_cast<uint16_t *>(ws + l.dg_off), *dU = reinterpret_cast<uint16_t *>(ws + l.du_off);
     const GradPlan plan = grad_plan(std::max<int64_t>(T, 1), D, F);
-    const GradStep dw = problems ? grad_step(problems, F, D, std::max<int64_t>(1, cdiv(T, 64))) : GradStep{};
+    const GradStep dw = problems ? grad_weight_step(problems, T, D, F) : GradStep{};
     if ((rc = clear_counters(fresh, std::max({plan.dh.counters, plan.dx.counters, dw.counters}), ws, l.fwd, st)))
         return rc;
 
@@ -245,7 +257,7 @@ int gmlp_train_backward(const void *dY, const void *X, const void *Wg, const voi
         p.M[0] = (int)F;
         p.N[0] = (int)T;
         p.K = (int)D;
-        p.problem_tiles = plan.dh.tiles;
+        p.problem_tiles = (int)plan.dh.tiles;
         p.g = bf16(G);
         p.u = bf16(U);
         p.dg = dG;
@@ -264,8 +276,7 @@ int gmlp_train_backward(const void *dY, const void *X, const void *Wg, const voi
         p.M[0] = (int)D;
         p.N[0] = (int)T;
         p.K = (int)F;
-        p.kt_seg = (int)cdiv(F, 64);
-        p.problem_tiles = plan.dx.tiles;
+        p.problem_tiles = (int)plan.dx.tiles;
         if ((rc = launch_grad<true, GRAD_STORE, 2>(plan.dx, p, "dX launch", st)))
             return rc;
     }
@@ -286,7 +297,7 @@ int gmlp_train_backward(const void *dY, const void *X, const void *Wg, const voi
         add(dU, X, dWu, F, D);
         add(dY, H, dWd, D, F);
         p.K = (int)T;
-        p.problem_tiles = dw.tiles / problems;
+        p.problem_tiles = (int)(dw.tiles / problems);
         if ((rc = launch_grad<false, GRAD_STORE, 1>(dw, p, "weight gradient launch", st)))
             return rc;
     }

@@ -4,16 +4,16 @@ Bounds.  Every output is an fp32 sum of products of bf16 numbers, rounded once
 to bf16 (relative error at most 2^-8 of the value; half a step).  Before that:
 
   * G and U have no other rounding than fp32 sums of K products: an error of at
-    most K 2^-24 sum |terms|, taken as K <= 4096 terms, 2^-12 sum |terms|
-    (worst case; the sums are random).
+    most K 2^-24 sum |terms|, with K <= 4104, 2^-12 sum |terms| (worst case; the
+    sums are random).  dX sums 2 F <= 16400 products, whose worst case, 2^-10, is
+    below the 2^-8 for the rounding of its operands that S carries in full.
   * Y = H Wd with H rounded to bf16: sum |H| |Wd| 2^-8.
   * dX, dWg, dWu: dG and dU rounded to bf16, likewise; dWd: H.
   * act and act' in fp32: exp and rcp to 2 units in the last place, 2^-20 is ample.
 
 So each output is within  2^-8 |ref| + (2^-8 + 2^-12 + 2^-20) S (1 + 2^-8),  S the
 sum of the absolute values of its terms, with the last factor for the terms of
-second order; 1.02 * 2^-8 * S + 2^-8 |ref| covers them at the sizes used (K up to
-4096), and 2^-12 S + 2^-8 |ref| where no operand was rounded.
+second order; 1.02 * 2^-8 * S + 2^-8 |ref| covers them at the sizes used, and 2^-12 S + 2^-8 |ref| where no operand was rounded.
 """
 import numpy as np
 import pytest
@@ -49,7 +49,7 @@ def inputs(T, D, F, seed):
 
 
 def check(name, got, ref, terms, rounded=True):
-    got = got.cpu().double()
+    got = got.double()
     assert got.shape == ref.shape, name
     bound = HALF_STEP * ref.abs() + (ROUNDED if rounded else 2.0 ** -12) * terms + 1e-30
     ratio = ((got - ref).abs() / bound).max().item() if ref.numel() else 0.0
@@ -65,7 +65,7 @@ def run(T, D, F, activation="silu", beta=1.0, seed=0, want=train.GRADIENTS, work
     y, g, u = train.forward(dev["x"], dev["wg"], dev["wu"], dev["wd"], **kw)
     grads = train.backward(dev["dy"], dev["x"], dev["wg"], dev["wu"], dev["wd"], g, u, want=want, **kw)
     torch.cuda.synchronize()
-    d = {k: v.double() for k, v in t.items()}
+    d = {k: v.double() for k, v in dev.items()}  # plain 64-bit matrix products
     check("g", g, d["x"] @ d["wg"], d["x"].abs() @ d["wg"].abs(), rounded=False)
     check("u", u, d["x"] @ d["wu"], d["x"].abs() @ d["wu"].abs(), rounded=False)
     # Y from the unrounded G and U.
@@ -76,7 +76,7 @@ def run(T, D, F, activation="silu", beta=1.0, seed=0, want=train.GRADIENTS, work
         (d["x"].abs() @ torch.maximum(d["wg"].abs(), d["wu"].abs()))
     check("y", y, h @ d["wd"], (h.abs() + 2.0 ** 8 * slack) @ d["wd"].abs())
     # The backward pass from the G and U it was given.
-    gd, ud = g.cpu().double(), u.cpu().double()
+    gd, ud = g.double(), u.double()
     a, da = act(gd, activation, beta)
     dh, dh_terms = d["dy"] @ d["wd"].T, d["dy"].abs() @ d["wd"].abs().T
     dg, du, h = dh * ud * da, dh * a, a * ud
@@ -109,10 +109,23 @@ def test_activations(T, D, F, activation, beta):
     run(T, D, F, activation, beta, seed=T)
 
 
-@pytest.mark.parametrize("T,D,F", [(260, 2048, 4096), (1029, 1288, 2312)])
-def test_large_tiles(T, D, F):
-    names = [k[0] for k in train.describe(T, D, F)]
-    assert any("<4, 2, 2, 4, 2>" in n for n in names), names
+# (T, D, F, tile of dH, of dX, of dW): every tile of the plan, most of them with
+# whole tiles, ragged ones and split sums.
+LARGE, PAIR, SMALL, T32, T64, T96, T160, T192, T320 = (
+    "4, 2, 2, 4, 2, 64, 1", "2, 2, 2, 4, 2, 32, 2", "2, 2, 2, 2, 4, 64, 1", "4, 1, 1, 1, 4, 64, 1", "4, 1, 1, 2, 4, 64, 1",
+    "4, 1, 1, 3, 4, 64, 1", "4, 1, 1, 5, 4, 64, 1", "4, 1, 1, 6, 3, 64, 1", "4, 2, 1, 5, 2, 64, 1")
+TILES = [(3, 264, 520, T32, T32, PAIR), (260, 264, 520, None, None, SMALL), (1030, 520, 1032, T64, None, None),
+         (1030, 1032, 2056, T96, SMALL, None), (600, 520, 1032, None, T64, None), (330, 1288, 2312, None, T96, None),
+         (400, 2056, 4104, None, T160, None), (520, 2056, 4104, None, T192, None), (40, 2056, 8200, T64, None, None),
+         (130, 4104, 8200, T160, T160, None), (180, 4104, 8200, T192, T192, None), (300, 4104, 8200, T320, T320, None),
+         (100, 4104, 8200, SMALL, None, None), (600, 4104, 8200, LARGE, None, None), (400, 4104, 8200, None, LARGE, None),
+         (2100, 2056, 8200, None, None, LARGE)]
+
+
+@pytest.mark.parametrize("T,D,F,dh,dx,dw", TILES, ids=["T%dD%dF%d" % c[:3] for c in TILES])
+def test_tiles(T, D, F, dh, dx, dw):
+    names = [k[0].split("Shape<")[1].split(">")[0] for k in train.describe(T, D, F)]
+    assert all(want in (None, have) for want, have in zip((dh, dx, dw), names)), names
     run(T, D, F, seed=3)
 
 
