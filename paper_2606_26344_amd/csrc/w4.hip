@@ -4,9 +4,10 @@
 
 #include <algorithm>
 #include <cmath>
+#include <initializer_list>
 
 #include "gmlp_w4.h"
-#include "hip_status.hpp"
+#include "launch.hpp"
 #include "w4.hpp"
 
 using namespace gmlp;
@@ -68,8 +69,48 @@ int check_w4_path(int path)
                : fail(GMLP_ERR_INVALID_ARG, "4-bit products have the automatic path only (got %d)", path);
 }
 
-// The counter block of every workspace, then H [T, F].
-size_t w4_workspace(int64_t T, int64_t D, int64_t F) { return kCounterBytes + align_up((size_t)std::max<int64_t>(T, 1) * std::max(D, F) * 2); }
+// The launch of one product: column strips of `ct` tiles, split over k where there
+// are too few of them to fill the chip and each piece keeps work for its waves.
+struct W4Step {
+    int tokens = 4; // rounded up: the kernel's
+    int ct = 1, strips = 0, splits = 1, split_ktiles = 0;
+    size_t partial_bytes = 0;
+};
+
+constexpr int kW4Waves = 8;
+constexpr int w4_ct(int tok) { return tok == 4 ? 1 : 2; }
+constexpr int w4_depth(int tok) { return tok == 4 ? 4 : tok <= 32 ? 2 : 1; }
+
+W4Step w4_step(int64_t T, int64_t K, int64_t N, int weights)
+{
+    W4Step s;
+    s.tokens = T <= 4 ? 4 : T <= 8 ? 8 : (int)cdiv(T, 16) * 16;
+    const int64_t ktiles = cdiv(K, 128), tiles = cdiv(N, 16);
+    s.ct = w4_ct(s.tokens);
+    s.strips = (int)cdiv(tiles, s.ct);
+    if (s.strips < kBlockTarget)
+        s.splits = (int)std::max<int64_t>(1, std::min<int64_t>(kBlockTarget / s.strips, ktiles / (2 * kW4Waves)));
+    s.split_ktiles = (int)cdiv(ktiles, s.splits);
+    s.splits = (int)cdiv(ktiles, s.split_ktiles);
+    const size_t slots = (size_t)weights * s.ct * std::max(1, s.tokens / 16) * (s.tokens < 16 ? s.tokens / 4 : 4);
+    s.partial_bytes = s.splits > 1 ? (size_t)s.splits * s.strips * slots * 64 * sizeof(float) : 0;
+    return s;
+}
+
+// The counter block of every workspace, H [T, F], then the partial sums of any step.
+struct W4Layout {
+    size_t partial = 0, total = 0;
+};
+
+W4Layout w4_workspace(int64_t T, int64_t D, int64_t F)
+{
+    T = std::max<int64_t>(T, 1);
+    W4Layout l;
+    l.partial = kCounterBytes + align_up((size_t)T * std::max(D, F) * 2);
+    l.total = l.partial + align_up(std::max({w4_step(T, D, F, 2).partial_bytes, w4_step(T, D, F, 1).partial_bytes,
+                                             w4_step(T, F, D, 2).partial_bytes, w4_step(T, F, D, 1).partial_bytes}));
+    return l;
+}
 
 int check_w4_workspace(void *ws, size_t bytes, size_t need)
 {
@@ -82,41 +123,30 @@ int check_w4_workspace(void *ws, size_t bytes, size_t need)
     return GMLP_OK;
 }
 
-constexpr int kW4Waves = 8;
-
-template <int TOK, int NW, int CT, int GPT, bool ZEROS>
+template <int TOK, int NW, int GPT, bool ZEROS>
 int launch_w4(const W4Params &p, hipStream_t st)
 {
-    constexpr int DEPTH = TOK > 32 ? 1 : TOK > 16 ? 2 : NW * CT >= 4 ? 2 : NW * CT == 2 ? 3 : 4;
-    hipLaunchKernelGGL((w4_kernel<TOK, NW, CT, GPT, ZEROS, kW4Waves, DEPTH>), dim3((unsigned)cdiv(p.N, 16 * CT)),
+    hipLaunchKernelGGL((w4_kernel<TOK, NW, w4_ct(TOK), GPT, ZEROS, kW4Waves, w4_depth(TOK)>), dim3((unsigned)(p.strips * p.splits)),
                        dim3(kW4Waves * 64), 0, st, p);
     return hip_check(hipGetLastError(), "4-bit product launch");
-}
-
-template <int TOK, int NW, int GPT, bool ZEROS>
-int launch_w4_width(const W4Params &p, hipStream_t st)
-{
-    if constexpr (NW == 1)
-        if (cdiv(p.N, 32) < kBlockTarget)
-            return launch_w4<TOK, 1, 1, GPT, ZEROS>(p, st);
-    return launch_w4<TOK, NW, 2, GPT, ZEROS>(p, st);
 }
 
 template <int TOK, int NW>
 int launch_w4_group(const W4Params &p, int group, bool zeros, hipStream_t st)
 {
     switch (group) {
-    case 32: return zeros ? launch_w4_width<TOK, NW, 4, true>(p, st) : launch_w4_width<TOK, NW, 4, false>(p, st);
-    case 64: return zeros ? launch_w4_width<TOK, NW, 2, true>(p, st) : launch_w4_width<TOK, NW, 2, false>(p, st);
-    default: return zeros ? launch_w4_width<TOK, NW, 1, true>(p, st) : launch_w4_width<TOK, NW, 1, false>(p, st);
+    case 32: return zeros ? launch_w4<TOK, NW, 4, true>(p, st) : launch_w4<TOK, NW, 4, false>(p, st);
+    case 64: return zeros ? launch_w4<TOK, NW, 2, true>(p, st) : launch_w4<TOK, NW, 2, false>(p, st);
+    default: return zeros ? launch_w4<TOK, NW, 1, true>(p, st) : launch_w4<TOK, NW, 1, false>(p, st);
     }
 }
 
 template <int NW>
 int run_w4(const void *X, const void *const (&packed)[2], void *out, int64_t T, int64_t K, int64_t N, int group, bool zeros,
-           int activation, float beta, hipStream_t st)
+           int activation, float beta, void *workspace, const W4Layout &ws, hipStream_t st)
 {
     const W4Packed l = w4_packed(K, N, group, zeros);
+    const W4Step s = w4_step(T, K, N, NW);
     W4Params p{};
     p.x = static_cast<const uint16_t *>(X);
     for (int w = 0; w < NW; ++w) {
@@ -125,19 +155,35 @@ int run_w4(const void *X, const void *const (&packed)[2], void *out, int64_t T, 
         p.zeros[w] = p.tiles[w] + l.zeros;
     }
     p.out = static_cast<uint16_t *>(out);
+    p.partial = reinterpret_cast<float *>(static_cast<uint8_t *>(workspace) + ws.partial);
+    p.counters = static_cast<uint32_t *>(workspace);
     p.T = (int)T;
     p.K = (int)K;
     p.N = (int)N;
     p.ktiles = (int)l.ktiles;
+    p.strips = s.strips;
+    p.splits = s.splits;
+    p.split_ktiles = s.split_ktiles;
     p.activation = activation;
     p.beta = beta;
-    if (T <= 4)
-        return launch_w4_group<4, NW>(p, group, zeros, st);
-    if (T <= 16)
-        return launch_w4_group<16, NW>(p, group, zeros, st);
-    if (T <= 32)
-        return launch_w4_group<32, NW>(p, group, zeros, st);
-    return launch_w4_group<64, NW>(p, group, zeros, st);
+    switch (s.tokens) {
+    case 4: return launch_w4_group<4, NW>(p, group, zeros, st);
+    case 8: return launch_w4_group<8, NW>(p, group, zeros, st);
+    case 16: return launch_w4_group<16, NW>(p, group, zeros, st);
+    case 32: return launch_w4_group<32, NW>(p, group, zeros, st);
+    case 48: return launch_w4_group<48, NW>(p, group, zeros, st);
+    default: return launch_w4_group<64, NW>(p, group, zeros, st);
+    }
+}
+
+// The counters that a call's products use, cleared for a workspace that has not
+// been prepared.
+int clear_w4_counters(int path, std::initializer_list<W4Step> steps, void *workspace, hipStream_t st)
+{
+    int words = 0;
+    for (const W4Step &s : steps)
+        words = std::max(words, s.splits > 1 ? s.strips : 0);
+    return path & GMLP_FRESH_WORKSPACE ? clear_words(static_cast<uint32_t *>(workspace), words, st) : GMLP_OK;
 }
 
 W4LayoutParams w4_layout_params(void *packed, int64_t K, int64_t N, int group, int zeros)
@@ -228,7 +274,7 @@ size_t gmlp_w4_workspace_size(int64_t T, int64_t D, int64_t F)
 {
     if (check_w4_tokens(T) || check_smm_shape(0, D, F))
         return 0;
-    return w4_workspace(T, D, F);
+    return w4_workspace(T, D, F).total;
 }
 
 int gmlp_w4_matmul(const void *X, const void *packed, void *Y, int64_t T, int64_t K, int64_t N, int group, int zeros,
@@ -241,15 +287,19 @@ int gmlp_w4_matmul(const void *X, const void *packed, void *Y, int64_t T, int64_
         return rc;
     if (!rows)
         return ok();
-    const size_t need = w4_workspace(T, K, N), yb = 2 * (size_t)T * N;
+    const W4Layout l = w4_workspace(T, K, N);
+    const size_t need = l.total, yb = 2 * (size_t)T * N;
     if ((rc = check_w4_workspace(workspace, ws_bytes, need)))
         return rc;
     if (overlaps(Y, yb, X, 2 * (size_t)T * K) || overlaps(Y, yb, packed, w4_packed(K, N, group, zeros).total) ||
         overlaps(Y, yb, workspace, need))
         return fail(GMLP_ERR_INVALID_ARG, "Y overlaps an input or the workspace");
     const void *const w[2] = {packed, nullptr};
-    rc = run_w4<1>(X, w, Y, T, K, N, group, zeros, 0, 1.0f, static_cast<hipStream_t>(stream));
-    return rc ? rc : ok();
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if ((rc = clear_w4_counters(path, {w4_step(T, K, N, 1)}, workspace, st)) ||
+        (rc = run_w4<1>(X, w, Y, T, K, N, group, zeros, 0, 1.0f, workspace, l, st)))
+        return rc;
+    return ok();
 }
 
 int gmlp_w4_gate_up(const void *X, const void *packed_g, const void *packed_u, void *H, int64_t T, int64_t D, int64_t F,
@@ -265,15 +315,19 @@ int gmlp_w4_gate_up(const void *X, const void *packed_g, const void *packed_u, v
         return rc;
     if (!rows)
         return ok();
-    const size_t need = w4_workspace(T, D, F), hb = 2 * (size_t)T * F, pb = w4_packed(D, F, group, zeros).total;
+    const W4Layout l = w4_workspace(T, D, F);
+    const size_t need = l.total, hb = 2 * (size_t)T * F, pb = w4_packed(D, F, group, zeros).total;
     if ((rc = check_w4_workspace(workspace, ws_bytes, need)))
         return rc;
     if (overlaps(H, hb, X, 2 * (size_t)T * D) || overlaps(H, hb, packed_g, pb) || overlaps(H, hb, packed_u, pb) ||
         overlaps(H, hb, workspace, need))
         return fail(GMLP_ERR_INVALID_ARG, "H overlaps an input or the workspace");
     const void *const w[2] = {packed_g, packed_u};
-    rc = run_w4<2>(X, w, H, T, D, F, group, zeros, v.act, v.beta, static_cast<hipStream_t>(stream));
-    return rc ? rc : ok();
+    hipStream_t st = static_cast<hipStream_t>(stream);
+    if ((rc = clear_w4_counters(path, {w4_step(T, D, F, 2)}, workspace, st)) ||
+        (rc = run_w4<2>(X, w, H, T, D, F, group, zeros, v.act, v.beta, workspace, l, st)))
+        return rc;
+    return ok();
 }
 
 int gmlp_w4_forward(const void *X, const void *packed_g, const void *packed_u, const void *packed_d, void *Y, int64_t T,
@@ -290,7 +344,8 @@ int gmlp_w4_forward(const void *X, const void *packed_g, const void *packed_u, c
         return rc;
     if (!rows)
         return ok();
-    const size_t need = w4_workspace(T, D, F), yb = 2 * (size_t)T * D;
+    const W4Layout l = w4_workspace(T, D, F);
+    const size_t need = l.total, yb = 2 * (size_t)T * D;
     const size_t gb = w4_packed(D, F, group, zeros).total, db = w4_packed(F, D, group, zeros).total;
     if ((rc = check_w4_workspace(workspace, ws_bytes, need)))
         return rc;
@@ -300,8 +355,9 @@ int gmlp_w4_forward(const void *X, const void *packed_g, const void *packed_u, c
     hipStream_t st = static_cast<hipStream_t>(stream);
     void *H = static_cast<uint8_t *>(workspace) + kCounterBytes;
     const void *const gu[2] = {packed_g, packed_u}, *const dn[2] = {packed_d, nullptr};
-    if ((rc = run_w4<2>(X, gu, H, T, D, F, group, zeros, v.act, v.beta, st)) ||
-        (rc = run_w4<1>(H, dn, Y, T, F, D, group, zeros, 0, 1.0f, st)))
+    if ((rc = clear_w4_counters(path, {w4_step(T, D, F, 2), w4_step(T, F, D, 1)}, workspace, st)) ||
+        (rc = run_w4<2>(X, gu, H, T, D, F, group, zeros, v.act, v.beta, workspace, l, st)) ||
+        (rc = run_w4<1>(H, dn, Y, T, F, D, group, zeros, 0, 1.0f, workspace, l, st)))
         return rc;
     return ok();
 }

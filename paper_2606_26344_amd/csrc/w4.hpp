@@ -20,9 +20,10 @@
 // 4 (e / 2) + 16 (e % 2).  So a wave streams 1 KB per load, in order, straight
 // into registers.  Scales [tile][column][group of the tile], zero points likewise.
 //
-// A block of WAVES waves computes CT column tiles (of both weights for gate/up),
-// each wave a contiguous range of the k-tiles; the waves' sums are added in
-// order through LDS.
+// A block of 4 or 8 waves computes CT column tiles (of both weights for gate/up),
+// each wave a contiguous range of the block's k-tiles with several of them in flight;
+// the waves' sums are added in order through LDS, and where there are few column
+// tiles those of several blocks over k through the workspace.
 #pragma once
 
 #include "common.hpp"
@@ -34,8 +35,12 @@ struct W4Params {
     const uint8_t *tiles[2]; // packed weights
     const uint8_t *scales[2], *zeros[2];
     uint16_t *out;           // [T, N]
+    float *partial;          // [split][strip][slot][lane]
+    uint32_t *counters;      // one per strip, zero on entry and exit
     int T, K, N;
     int ktiles;              // tiles of 128 rows
+    int strips, splits;      // column strips of CT tiles; blocks over k of each
+    int split_ktiles;        // k-tiles of a block
     int activation;
     float beta;
 };
@@ -75,43 +80,65 @@ __device__ __forceinline__ bf16x8 w4_unpack(uint32_t d)
                                             (d >> 8 & kW4Nibbles) | kW4One, (d >> 12 & kW4Nibbles) | kW4One});
 }
 
-// TOK: tokens, rounded up to 4, 16, 32 or 64.  GPT: groups per k-tile (128 /
-// group).  DEPTH: k-tiles of a wave in flight.
+// TOK: tokens, rounded up to 4, 8 or a multiple of 16.  GPT: scale groups per k-tile
+// (128 / group).  DEPTH: k-tiles of a wave in flight.
+//
+// Up to 8 tokens the rows of a k-tile, 1 or 2 KB, are loaded as they lie and reach
+// the MFMA layout through LDS: loaded in that layout, with 16 lanes for every token
+// that is not there, they would take four times the weights' loads.
 template <int TOK, int NW, int CT, int GPT, bool ZEROS, int WAVES, int DEPTH>
-__global__ __launch_bounds__(WAVES * 64) void w4_kernel(W4Params p)
+__global__ __launch_bounds__(WAVES * 64, 8 / WAVES) void w4_kernel(W4Params p)
 {
     constexpr int NB = (TOK + 15) / 16, NR = TOK >= 16 ? 4 : TOK / 4, MPG = 4 / GPT;
-    constexpr int SLOTS = NW * CT * NB * NR;
+    constexpr int SLOTS = NW * CT * NB * NR; // results per lane
+    constexpr bool VIA_LDS = TOK <= 8;
+    constexpr int X_REGS = VIA_LDS ? TOK / 4 : NB * 4; // 16-byte registers of a k-tile of X
     using Group = W4Group<GPT>;
     __shared__ float part[WAVES * SLOTS * 64];
+    __shared__ __attribute__((aligned(256))) uint8_t rows[VIA_LDS ? WAVES * TOK * 256 : 16];
+    __shared__ int s_last;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-    const int K = p.K, ktiles = p.ktiles;
-    const int ntiles = (p.N + 15) >> 4;
-    const int first = blockIdx.x * CT;
-    const int per = (ktiles + WAVES - 1) / WAVES;
-    const int begin = wave * per, end = min(ktiles, begin + per);
+    const int K = p.K, ntiles = (p.N + 15) >> 4;
+    const int strip = blockIdx.x % p.strips, split = blockIdx.x / p.strips;
+    const int first = strip * CT;
+    const int split_begin = split * p.split_ktiles, split_end = min(p.ktiles, split_begin + p.split_ktiles);
+    const int per = (split_end - split_begin + WAVES - 1) / WAVES;
+    const int begin = split_begin + wave * per, end = min(split_end, begin + per);
 
-    // Row r of operand A is token r / 4 + 4 (r % 4) of its 16; tokens past T
-    // repeat the last one and feed results that are not stored.
+    // Row r of operand A is token r / 4 + 4 (r % 4) of its 16.  Tokens past T repeat
+    // the last one and feed results that are not stored.
     const __amdgpu_buffer_rsrc_t rx = make_rsrc(p.x);
     const int kq = lane >> 4, row = lane & 15;
-    uint32_t x_off[NB];
+    uint32_t x_off[VIA_LDS ? X_REGS : NB];
+    int x_read = 0, x_write = 0;
+    if constexpr (VIA_LDS) {
+        // Register i: token 4 i + lane / 16, chunk lane % 16 (8 k).  In LDS a token's
+        // chunks are XORed with the token so that the reads of different tokens
+        // do not meet on a bank.
 #pragma unroll
-    for (int nb = 0; nb < NB; ++nb)
-        x_off[nb] = ((uint32_t)min(16 * nb + (row >> 2) + 4 * (row & 3), p.T - 1) * (uint32_t)K + 8u * kq) * 2u;
+        for (int i = 0; i < X_REGS; ++i)
+            x_off[i] = ((uint32_t)min(4 * i + kq, p.T - 1) * (uint32_t)K + 8u * row) * 2u;
+        const int t = (row >> 2) + 4 * ((row & 3) % NR);
+        x_write = wave * TOK * 256 + kq * 256 + ((row ^ kq << 2) << 4);
+        x_read = wave * TOK * 256 + t * 256 + ((kq ^ (t & 3) << 2) << 4);
+    } else {
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+            x_off[nb] = ((uint32_t)min(16 * nb + (row >> 2) + 4 * (row & 3), p.T - 1) * (uint32_t)K + 8u * kq) * 2u;
+    }
     size_t tile[CT];
 #pragma unroll
     for (int c = 0; c < CT; ++c)
-        tile[c] = (size_t)min(first + c, ntiles - 1) * ktiles;
+        tile[c] = (size_t)min(first + c, ntiles - 1) * p.ktiles;
 
     struct Batch {
         u32x4 w[NW][CT];
         typename Group::scales s[NW][CT];
         typename Group::zeros z[ZEROS ? NW : 1][ZEROS ? CT : 1];
-        bf16x8 x[NB][4];
+        u32x4 x[X_REGS];
     };
     auto load = [&](Batch &b, int kt) __attribute__((always_inline)) {
-        kt = min(kt, ktiles - 1); // past the end: loaded, not used
+        kt = min(kt, p.ktiles - 1); // past the end: loaded, not used
 #pragma unroll
         for (int w = 0; w < NW; ++w)
 #pragma unroll
@@ -123,19 +150,33 @@ __global__ __launch_bounds__(WAVES * 64) void w4_kernel(W4Params p)
                     b.z[w][c] = ((const typename Group::zeros *)p.zeros[w])[at * 16 + row];
             }
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int k = kt * 128 + 32 * j; // rows past K multiply zeros
-                const uint32_t off = k + 8 * kq < K ? x_off[nb] + (uint32_t)k * 2u : kOutOfRange;
-                b.x[nb][j] = __builtin_bit_cast(bf16x8, __builtin_amdgcn_raw_buffer_load_b128(rx, off, 0, 0));
-            }
+        for (int i = 0; i < X_REGS; ++i) {
+            // Columns of X past K read as zeros: rows past K of the weight count
+            // for nothing.
+            const int k = kt * 128 + (VIA_LDS ? 0 : 32 * (i % 4));
+            const uint32_t off = k + 8 * (VIA_LDS ? row : kq) < K ? x_off[VIA_LDS ? i : i / 4] + (uint32_t)k * 2u : kOutOfRange;
+            b.x[i] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rx, off, 0, 0));
+        }
     };
     float total[NW][CT][NB][NR] = {};
     const auto constant = [](uint32_t v) __attribute__((always_inline)) {
         return __builtin_bit_cast(bf16x8, u32x4{v, v, v, v});
     };
     auto use = [&](const Batch &b) __attribute__((always_inline)) {
+        bf16x8 x[NB][4];
+        if constexpr (VIA_LDS) {
+            // The wave's own rows: its LDS operations run in order.
+#pragma unroll
+            for (int i = 0; i < X_REGS; ++i)
+                *(u32x4 *)(rows + x_write + i * 1024) = b.x[i];
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                x[0][j] = *(const bf16x8 *)(rows + (x_read ^ j << 6));
+        } else {
+#pragma unroll
+            for (int i = 0; i < X_REGS; ++i)
+                x[i / 4][i % 4] = __builtin_bit_cast(bf16x8, b.x[i]);
+        }
 #pragma unroll
         for (int g = 0; g < GPT; ++g) {
             f32x4 mid[NB];
@@ -145,7 +186,7 @@ __global__ __launch_bounds__(WAVES * 64) void w4_kernel(W4Params p)
                     mid[nb] = f32x4{};
 #pragma unroll
                     for (int m = 0; m < MPG; ++m)
-                        mid[nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b.x[nb][g * MPG + m], constant(kW4MinusMid),
+                        mid[nb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[nb][g * MPG + m], constant(kW4MinusMid),
                                                                           mid[nb], 0, 0, 0);
                 }
 #pragma unroll
@@ -165,14 +206,14 @@ __global__ __launch_bounds__(WAVES * 64) void w4_kernel(W4Params p)
                             acc = f32x4{};
 #pragma unroll
                             for (int m = 0; m < MPG; ++m)
-                                acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b.x[nb][g * MPG + m], constant(z | z << 16),
+                                acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[nb][g * MPG + m], constant(z | z << 16),
                                                                               acc, 0, 0, 0);
                         } else {
                             acc = mid[nb];
                         }
 #pragma unroll
                         for (int m = 0; m < MPG; ++m)
-                            acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(b.x[nb][g * MPG + m], q[m], acc, 0, 0, 0);
+                            acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[nb][g * MPG + m], q[m], acc, 0, 0, 0);
 #pragma unroll
                         for (int i = 0; i < NR; ++i)
                             total[w][c][nb][i] += s * acc[i];
@@ -186,7 +227,7 @@ __global__ __launch_bounds__(WAVES * 64) void w4_kernel(W4Params p)
     for (int d = 0; d < DEPTH; ++d)
         load(batch[d], begin + d);
     int kt = begin;
-    for (; kt + DEPTH <= end; kt += DEPTH)
+    for (; kt + DEPTH < end; kt += DEPTH)
 #pragma unroll
         for (int d = 0; d < DEPTH; ++d) {
             use(batch[d]);
@@ -208,15 +249,51 @@ __global__ __launch_bounds__(WAVES * 64) void w4_kernel(W4Params p)
                 for (int i = 0; i < NR; ++i)
                     part[(wave * SLOTS + ((w * CT + c) * NB + nb) * NR + i) * 64 + lane] = total[w][c][nb][i];
     __syncthreads();
+    auto block_sum = [&](int slot) __attribute__((always_inline)) {
+        float v = part[slot * 64 + lane];
+#pragma unroll
+        for (int o = 1; o < WAVES; ++o)
+            v += part[(o * SLOTS + slot) * 64 + lane];
+        return v;
+    };
+    // ---- and of the blocks over k -------------------------------------------------
+    // Written through to memory (device-coherent), counted in, and added in order by
+    // the last block of the strip.
+    const __amdgpu_buffer_rsrc_t prs = make_rsrc(p.partial);
+    auto partial_at = [&](int sp, int slot) __attribute__((always_inline)) {
+        return (uint32_t)((sp * p.strips + strip) * SLOTS + slot) * 256u;
+    };
+    if (p.splits > 1) {
+        for (int slot = wave; slot < SLOTS; slot += WAVES)
+            __builtin_amdgcn_raw_buffer_store_b32(__builtin_bit_cast(uint32_t, block_sum(slot)), prs, lane * 4,
+                                                  partial_at(split, slot), kCoherent);
+        wait_vmcnt<0>();
+        __syncthreads();
+        if (tid == 0) {
+            const uint32_t before =
+                __hip_atomic_fetch_add(p.counters + strip, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            s_last = before == (uint32_t)(p.splits - 1);
+        }
+        __syncthreads();
+        if (!s_last)
+            return;
+        if (tid == 0)
+            __hip_atomic_store(p.counters + strip, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+    }
     constexpr int OUT = CT * NB * NR; // result slots of one weight
     for (int slot = wave; slot < OUT; slot += WAVES) {
         float v[NW];
 #pragma unroll
         for (int w = 0; w < NW; ++w) {
-            v[w] = part[(w * OUT + slot) * 64 + lane];
-#pragma unroll
-            for (int o = 1; o < WAVES; ++o)
-                v[w] += part[(o * SLOTS + w * OUT + slot) * 64 + lane];
+            const int at = w * OUT + slot;
+            if (p.splits > 1) {
+                v[w] = 0.0f;
+                for (int sp = 0; sp < p.splits; ++sp)
+                    v[w] += __builtin_bit_cast(float, (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(
+                                                          prs, lane * 4, partial_at(sp, at), kCoherent));
+            } else {
+                v[w] = block_sum(at);
+            }
             v[w] *= 128.0f; // the weights were (q - z) / 128
         }
         const int i = slot % NR, nb = slot / NR % NB, c = slot / (NR * NB);
