@@ -21,7 +21,7 @@ from typing import Optional
 
 import torch
 
-from .gmlp import _CALL_DEVICE, _check, _empty, _expect, _ptr, _scratch, _stream, library
+from .gmlp import _CALL_DEVICE, _check, _empty, _empty_like, _expect, _ptr, _scratch, _stream, library
 
 POST, RES_FP32, GATE_ROWS = 1, 2, 4
 
@@ -93,11 +93,11 @@ def forward(y: Optional[torch.Tensor], res: torch.Tensor, w_pre: Optional[torch.
     if y is not None:
         _expect(y, "y", (T, D), dev)
     if r is None:
-        r = _empty((T, D), dtype, dev, stream)
+        r = _empty_like(res, stream)
     else:
         _stream_tensor(r, "r", (T, D), dev, dtype)
     if xn is None:
-        xn = _empty((T, D), torch.bfloat16, dev, stream)
+        xn = _empty((T, D), torch.bfloat16, dev, stream) if y is None else _empty_like(y, stream)
     else:
         _expect(xn, "xn", (T, D), dev)
     _check(library().gmlp_block_norm(_ptr(y), res.data_ptr(), _ptr(w_pre), _ptr(w_post), _ptr(gate), r.data_ptr(),
@@ -121,17 +121,16 @@ def backward(dxn: torch.Tensor, dr: Optional[torch.Tensor], y: Optional[torch.Te
     if y is not None:
         _expect(y, "y", (T, D), dev)
         if dy is None:
-            dy = _empty((T, D), torch.bfloat16, dev, stream)
+            dy = _empty_like(y, stream)
         else:
             _expect(dy, "dy", (T, D), dev)
     elif dy is not None:
         raise ValueError("dy is given without y")
     if dres is None:
-        dres = _empty((T, D), dtype, dev, stream)
+        dres = _empty_like(r, stream)
     else:
         _stream_tensor(dres, "dres", (T, D), dev, dtype)
-    dw_pre, dw_post, dgate = (None if t is None else _empty(t.shape, torch.bfloat16, dev, stream)
-                              for t in (w_pre, w_post, gate))
+    dw_pre, dw_post, dgate = (None if t is None else _empty_like(t, stream) for t in (w_pre, w_post, gate))
     if workspace is None:
         nbytes = workspace_size(T, D)
         keep, ws = _scratch(nbytes, 1, _CALL_DEVICE, stream, False, "invalid shape T=%d D=%d" % (T, D))

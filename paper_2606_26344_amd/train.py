@@ -20,7 +20,7 @@ from typing import Optional, Sequence
 
 import torch
 
-from .gmlp import (_CALL_DEVICE, FRESH_WORKSPACE, PATH_AUTO, Workspace, _check, _empty, _expect, _parse_plan, _ptr,
+from .gmlp import (_CALL_DEVICE, FRESH_WORKSPACE, PATH_AUTO, Workspace, _check, _empty, _empty_like, _expect, _parse_plan, _ptr,
                    _scratch, _stream, _variant, library)
 
 GRADIENTS = ("dx", "dwg", "dwu", "dwd")
@@ -54,10 +54,11 @@ def _workspace(workspace, T, D, F, rows, stream):
     return keep, ws, n, PATH_AUTO | FRESH_WORKSPACE
 
 
-def _output(t, name, shape, device, stream):
+def _output(t, name, like, stream):
+    """The given output, or a new one, of the shape of a tensor already checked."""
     if t is None:
-        return _empty(shape, torch.bfloat16, device, stream)
-    _expect(t, name, shape, device)
+        return _empty_like(like, stream)
+    _expect(t, name, like.shape, like.device)
     return t
 
 
@@ -81,9 +82,11 @@ def forward(x: torch.Tensor, wg: torch.Tensor, wu: torch.Tensor, wd: torch.Tenso
     are for backward().  ``out``, ``g`` and ``u`` may be given to write into."""
     T, D, F, dev = _weights(x, wg, wu, wd)
     act, beta, _, _ = _variant(activation, beta, False, 0.0)
-    out = _output(out, "out", (T, D), dev, stream)
-    g = _output(g, "g", (T, F), dev, stream)
-    u = _output(u, "u", (T, F), dev, stream)
+    out = _output(out, "out", x, stream)
+    g = _empty((T, F), torch.bfloat16, dev, stream) if g is None else g
+    u = _empty_like(g, stream) if u is None else u
+    _expect(g, "g", (T, F), dev)
+    _expect(u, "u", (T, F), dev)
     keep, ws, nbytes, path = _workspace(workspace, T, D, F, T, stream)
     _check(library().gmlp_train_forward(x.data_ptr(), wg.data_ptr(), wu.data_ptr(), wd.data_ptr(), out.data_ptr(),
                                         g.data_ptr(), u.data_ptr(), T, D, F, act, beta, path, ws, nbytes,
@@ -104,14 +107,13 @@ def backward(dy: torch.Tensor, x: torch.Tensor, wg: torch.Tensor, wu: torch.Tens
     _expect(dy, "dy", (T, D), dev)
     _expect(g, "g", (T, F), dev)
     _expect(u, "u", (T, F), dev)
-    unknown = sorted(set(want) - set(GRADIENTS))
-    if unknown:
-        raise ValueError("want names %s, the gradients are %s" % (unknown, GRADIENTS))
+    if want is not GRADIENTS and set(want) - set(GRADIENTS):
+        raise ValueError("want names %s, the gradients are %s" % (sorted(set(want) - set(GRADIENTS)), GRADIENTS))
     act, beta, _, _ = _variant(activation, beta, False, 0.0)
     outs = []
-    for name, t, shape in (("dx", dx, (T, D)), ("dwg", dwg, (D, F)), ("dwu", dwu, (D, F)), ("dwd", dwd, (F, D))):
+    for name, t, like in (("dx", dx, x), ("dwg", dwg, wg), ("dwu", dwu, wu), ("dwd", dwd, wd)):
         if name in want:
-            outs.append(_output(t, name, shape, dev, stream))
+            outs.append(_output(t, name, like, stream))
         elif t is not None:
             raise ValueError("%s is given but not wanted" % name)
         else:
