@@ -69,31 +69,55 @@ int check_w4_path(int path)
                : fail(GMLP_ERR_INVALID_ARG, "4-bit products have the automatic path only (got %d)", path);
 }
 
-// The launch of one product: column strips of `ct` tiles, split over k where there
-// are too few of them to fill the chip and each piece keeps work for its waves.
+// The launch of one product: column strips, split over k where there are too few of
+// them to fill the chip and each piece keeps work for its waves.
 struct W4Step {
     int tokens = 4; // rounded up: the kernel's
-    int ct = 1, strips = 0, splits = 1, split_ktiles = 0;
+    bool shared = false;
+    int strips = 0, splits = 1, split_ktiles = 0;
     size_t partial_bytes = 0;
 };
 
+// The column tiles of a strip and the k-tiles a wave has asked for before it uses one.
+// One tile and 4 ahead for T <= 4 (D = 4096, F = 14336, T = 1: gate/up 14.6 us, down 7.6);
+// from there on two tiles, since X comes through LDS once for both, and 2 ahead, 1 where
+// more would not fit the registers (T = 33, D = 2048, F = 8192, groups of 32: 10.2 us and 12.8).
 constexpr int kW4Waves = 8;
 constexpr int w4_ct(int tok) { return tok == 4 ? 1 : 2; }
 constexpr int w4_depth(int tok) { return tok == 4 ? 4 : tok <= 32 ? 2 : 1; }
 
-W4Step w4_step(int64_t T, int64_t K, int64_t N, int weights)
+// The same for the kernel whose waves share X.
+constexpr int w4_shared_depth(int tok, int weights) { return weights == 1 ? 6 : tok <= 48 ? 4 : 2; }
+
+// The waves share X from 16 tokens on, if 16 k-tiles a block still fill three quarters
+// of the chip.  us shared against not, gate/up and down of D = 4096, F = 14336, groups of
+// 128: 15.0 against 17.6 and 13.4 against 13.7 at T = 16, 26.6 against 31.5 and 20.8
+// against 24.9 at 40, 31.1 against 43.2 and 24.2 against 32.5 at 64.  With 128 blocks of 16
+// k-tiles (D = 2048, F = 8192, T = 33) gate/up takes 19.7 against 10.6.  Groups of 32 gain
+// nothing, their scales cost the wave more than X: 35.9 against 33.1 and 26.1 against 26.8
+// at T = 40.
+constexpr int kW4SharedTokens = 16, kW4SharedTiles = 16, kW4SharedGroup = 64;
+
+W4Step w4_step(int64_t T, int64_t K, int64_t N, int weights, int group)
 {
     W4Step s;
     s.tokens = T <= 4 ? 4 : T <= 8 ? 8 : (int)cdiv(T, 16) * 16;
-    const int64_t ktiles = cdiv(K, 128), tiles = cdiv(N, 16);
-    s.ct = w4_ct(s.tokens);
-    s.strips = (int)cdiv(tiles, s.ct);
-    if (s.strips < kBlockTarget)
-        s.splits = (int)std::max<int64_t>(1, std::min<int64_t>(kBlockTarget / s.strips, ktiles / (2 * kW4Waves)));
-    s.split_ktiles = (int)cdiv(ktiles, s.splits);
-    s.splits = (int)cdiv(ktiles, s.split_ktiles);
-    const size_t slots = (size_t)weights * s.ct * std::max(1, s.tokens / 16) * (s.tokens < 16 ? s.tokens / 4 : 4);
-    s.partial_bytes = s.splits > 1 ? (size_t)s.splits * s.strips * slots * 64 * sizeof(float) : 0;
+    const int64_t ktiles = cdiv(K, 128);
+    auto split = [&](int64_t strips, int64_t least) {
+        s.strips = (int)strips;
+        s.splits = (int)std::max<int64_t>(1, std::min<int64_t>(kBlockTarget / strips, ktiles / least));
+        s.split_ktiles = (int)cdiv(ktiles, s.splits);
+        s.splits = (int)cdiv(ktiles, s.split_ktiles);
+    };
+    int columns = kW4SharedColumns;
+    split(cdiv(N, columns), kW4SharedTiles);
+    s.shared = s.tokens >= kW4SharedTokens && group >= kW4SharedGroup && s.split_ktiles >= kW4SharedTiles &&
+               s.strips * s.splits >= kBlockTarget * 3 / 4;
+    if (!s.shared) {
+        columns = 16 * w4_ct(s.tokens);
+        split(cdiv(N, columns), 2 * kW4Waves);
+    }
+    s.partial_bytes = s.splits > 1 ? (size_t)s.splits * s.strips * weights * s.tokens * columns * sizeof(float) : 0;
     return s;
 }
 
@@ -107,8 +131,12 @@ W4Layout w4_workspace(int64_t T, int64_t D, int64_t F)
     T = std::max<int64_t>(T, 1);
     W4Layout l;
     l.partial = kCounterBytes + align_up((size_t)T * std::max(D, F) * 2);
-    l.total = l.partial + align_up(std::max({w4_step(T, D, F, 2).partial_bytes, w4_step(T, D, F, 1).partial_bytes,
-                                             w4_step(T, F, D, 2).partial_bytes, w4_step(T, F, D, 1).partial_bytes}));
+    size_t partial = 0;
+    for (int group : {32, kW4SharedGroup})
+        for (int weights : {1, 2})
+            partial = std::max({partial, w4_step(T, D, F, weights, group).partial_bytes,
+                                w4_step(T, F, D, weights, group).partial_bytes});
+    l.total = l.partial + align_up(partial);
     return l;
 }
 
@@ -124,20 +152,27 @@ int check_w4_workspace(void *ws, size_t bytes, size_t need)
 }
 
 template <int TOK, int NW, int GPT, bool ZEROS>
-int launch_w4(const W4Params &p, hipStream_t st)
+int launch_w4(const W4Params &p, bool shared, hipStream_t st)
 {
-    hipLaunchKernelGGL((w4_kernel<TOK, NW, w4_ct(TOK), GPT, ZEROS, kW4Waves, w4_depth(TOK)>), dim3((unsigned)(p.strips * p.splits)),
+    const dim3 grid((unsigned)(p.strips * p.splits));
+    if constexpr (TOK >= kW4SharedTokens && 128 / GPT >= kW4SharedGroup)
+        if (shared) {
+            hipLaunchKernelGGL((w4_shared_kernel<TOK / 16, NW, GPT, ZEROS, w4_shared_depth(TOK, NW)>), grid,
+                               dim3(kW4SharedWaves * 64), 0, st, p);
+            return hip_check(hipGetLastError(), "4-bit product launch");
+        }
+    hipLaunchKernelGGL((w4_kernel<TOK, NW, w4_ct(TOK), GPT, ZEROS, kW4Waves, w4_depth(TOK)>), grid,
                        dim3(kW4Waves * 64), 0, st, p);
     return hip_check(hipGetLastError(), "4-bit product launch");
 }
 
 template <int TOK, int NW>
-int launch_w4_group(const W4Params &p, int group, bool zeros, hipStream_t st)
+int launch_w4_group(const W4Params &p, bool shared, int group, bool zeros, hipStream_t st)
 {
     switch (group) {
-    case 32: return zeros ? launch_w4<TOK, NW, 4, true>(p, st) : launch_w4<TOK, NW, 4, false>(p, st);
-    case 64: return zeros ? launch_w4<TOK, NW, 2, true>(p, st) : launch_w4<TOK, NW, 2, false>(p, st);
-    default: return zeros ? launch_w4<TOK, NW, 1, true>(p, st) : launch_w4<TOK, NW, 1, false>(p, st);
+    case 32: return zeros ? launch_w4<TOK, NW, 4, true>(p, shared, st) : launch_w4<TOK, NW, 4, false>(p, shared, st);
+    case 64: return zeros ? launch_w4<TOK, NW, 2, true>(p, shared, st) : launch_w4<TOK, NW, 2, false>(p, shared, st);
+    default: return zeros ? launch_w4<TOK, NW, 1, true>(p, shared, st) : launch_w4<TOK, NW, 1, false>(p, shared, st);
     }
 }
 
@@ -146,7 +181,7 @@ int run_w4(const void *X, const void *const (&packed)[2], void *out, int64_t T, 
            int activation, float beta, void *workspace, const W4Layout &ws, hipStream_t st)
 {
     const W4Packed l = w4_packed(K, N, group, zeros);
-    const W4Step s = w4_step(T, K, N, NW);
+    const W4Step s = w4_step(T, K, N, NW, group);
     W4Params p{};
     p.x = static_cast<const uint16_t *>(X);
     for (int w = 0; w < NW; ++w) {
@@ -167,12 +202,12 @@ int run_w4(const void *X, const void *const (&packed)[2], void *out, int64_t T, 
     p.activation = activation;
     p.beta = beta;
     switch (s.tokens) {
-    case 4: return launch_w4_group<4, NW>(p, group, zeros, st);
-    case 8: return launch_w4_group<8, NW>(p, group, zeros, st);
-    case 16: return launch_w4_group<16, NW>(p, group, zeros, st);
-    case 32: return launch_w4_group<32, NW>(p, group, zeros, st);
-    case 48: return launch_w4_group<48, NW>(p, group, zeros, st);
-    default: return launch_w4_group<64, NW>(p, group, zeros, st);
+    case 4: return launch_w4_group<4, NW>(p, s.shared, group, zeros, st);
+    case 8: return launch_w4_group<8, NW>(p, s.shared, group, zeros, st);
+    case 16: return launch_w4_group<16, NW>(p, s.shared, group, zeros, st);
+    case 32: return launch_w4_group<32, NW>(p, s.shared, group, zeros, st);
+    case 48: return launch_w4_group<48, NW>(p, s.shared, group, zeros, st);
+    default: return launch_w4_group<64, NW>(p, s.shared, group, zeros, st);
     }
 }
 
@@ -296,7 +331,7 @@ int gmlp_w4_matmul(const void *X, const void *packed, void *Y, int64_t T, int64_
         return fail(GMLP_ERR_INVALID_ARG, "Y overlaps an input or the workspace");
     const void *const w[2] = {packed, nullptr};
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if ((rc = clear_w4_counters(path, {w4_step(T, K, N, 1)}, workspace, st)) ||
+    if ((rc = clear_w4_counters(path, {w4_step(T, K, N, 1, group)}, workspace, st)) ||
         (rc = run_w4<1>(X, w, Y, T, K, N, group, zeros, 0, 1.0f, workspace, l, st)))
         return rc;
     return ok();
@@ -324,7 +359,7 @@ int gmlp_w4_gate_up(const void *X, const void *packed_g, const void *packed_u, v
         return fail(GMLP_ERR_INVALID_ARG, "H overlaps an input or the workspace");
     const void *const w[2] = {packed_g, packed_u};
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if ((rc = clear_w4_counters(path, {w4_step(T, D, F, 2)}, workspace, st)) ||
+    if ((rc = clear_w4_counters(path, {w4_step(T, D, F, 2, group)}, workspace, st)) ||
         (rc = run_w4<2>(X, w, H, T, D, F, group, zeros, v.act, v.beta, workspace, l, st)))
         return rc;
     return ok();
@@ -355,7 +390,7 @@ int gmlp_w4_forward(const void *X, const void *packed_g, const void *packed_u, c
     hipStream_t st = static_cast<hipStream_t>(stream);
     void *H = static_cast<uint8_t *>(workspace) + kCounterBytes;
     const void *const gu[2] = {packed_g, packed_u}, *const dn[2] = {packed_d, nullptr};
-    if ((rc = clear_w4_counters(path, {w4_step(T, D, F, 2), w4_step(T, F, D, 1)}, workspace, st)) ||
+    if ((rc = clear_w4_counters(path, {w4_step(T, D, F, 2, group), w4_step(T, F, D, 1, group)}, workspace, st)) ||
         (rc = run_w4<2>(X, gu, H, T, D, F, group, zeros, v.act, v.beta, workspace, l, st)) ||
         (rc = run_w4<1>(H, dn, Y, T, F, D, group, zeros, 0, 1.0f, workspace, l, st)))
         return rc;

@@ -305,6 +305,209 @@ __global__ __launch_bounds__(WAVES * 64, 8 / WAVES) void w4_kernel(W4Params p)
     }
 }
 
+// ---- more tokens: X shared by the waves of a block ----------------------------------
+// A block of 4 waves computes 64 columns (of both weights for gate/up), 16 per wave,
+// over all the block's k-tiles: for 16 tokens and more, where k is long.  A k-tile of X, 16 NB tokens, is loaded once by the
+// block and read by the four waves from LDS; it would otherwise be loaded in the MFMA
+// layout by every wave, 4 NB KB for each KB of a weight tile.  LDS holds two k-tiles, X
+// is XD of them ahead in registers and the weights DEPTH.  What bounds it is the MFMAs
+// (a third of them for the zero point) and the LDS reads of a step one after the other:
+// 2 blocks to a CU, or the two sums of a group in separate registers, gain nothing.
+//
+// LDS rows of one token, 16 chunks of 8 k, chunk c at position c ^ token % 16: the 16
+// lanes that read one chunk of 16 tokens meet all banks.
+constexpr int kW4SharedWaves = 4, kW4SharedColumns = 16 * kW4SharedWaves;
+template <int NB, int NW, int GPT, bool ZEROS, int DEPTH>
+__global__ __launch_bounds__(kW4SharedWaves * 64, 1) void w4_shared_kernel(W4Params p)
+{
+    constexpr int MPG = 4 / GPT, XD = 2;
+    using Group = W4Group<GPT>;
+    __shared__ __attribute__((aligned(256))) uint8_t rows[2][NB * 16 * 256];
+    __shared__ int s_last;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int K = p.K, ntiles = (p.N + 15) >> 4;
+    const int strip = blockIdx.x % p.strips, split = blockIdx.x / p.strips;
+    const int begin = split * p.split_ktiles, end = min(p.ktiles, begin + p.split_ktiles);
+    const int kq = lane >> 4, row = lane & 15;
+    const int column_tile = strip * kW4SharedWaves + wave;
+    const size_t tile = (size_t)min(column_tile, ntiles - 1) * p.ktiles;
+
+    // X: thread t brings chunk t % 16 of tokens t / 16 + 16 nb; tokens past T and
+    // columns past K read as zeros.
+    const __amdgpu_buffer_rsrc_t rx = make_rsrc(p.x);
+    const int x_token = tid >> 4, x_chunk = tid & 15;
+    const int x_write = x_token * 256 + ((x_chunk ^ x_token) << 4);
+    struct Rows {
+        u32x4 v[NB];
+    };
+    auto load_rows = [&](Rows &r, int kt) __attribute__((always_inline)) {
+        const int k = kt * 128 + x_chunk * 8;
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+            const int t = x_token + 16 * nb;
+            const uint32_t off = k < K && t < p.T ? ((uint32_t)t * (uint32_t)K + (uint32_t)k) * 2u : kOutOfRange;
+            r.v[nb] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rx, off, 0, 0));
+        }
+    };
+    auto store_rows = [&](const Rows &r, int stage) __attribute__((always_inline)) {
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+            *(u32x4 *)(rows[stage] + x_write + nb * 16 * 256) = r.v[nb];
+    };
+    const int x_read = row * 256 + ((kq ^ row) << 4); // chunk 4 j + kq: XOR 64 j
+
+    struct Batch {
+        u32x4 w[NW];
+        typename Group::scales s[NW];
+        typename Group::zeros z[ZEROS ? NW : 1];
+    };
+    auto load = [&](Batch &b, int kt) __attribute__((always_inline)) {
+        const size_t at = tile + min(kt, p.ktiles - 1); // past the end: loaded, not used
+#pragma unroll
+        for (int w = 0; w < NW; ++w) {
+            b.w[w] = __builtin_nontemporal_load((const u32x4 *)(p.tiles[w] + at * 1024 + lane * 16));
+            b.s[w] = ((const typename Group::scales *)p.scales[w])[at * 16 + row];
+            if constexpr (ZEROS)
+                b.z[w] = ((const typename Group::zeros *)p.zeros[w])[at * 16 + row];
+        }
+    };
+    f32x4 total[NW][NB] = {};
+    const auto constant = [](uint32_t v) __attribute__((always_inline)) {
+        return __builtin_bit_cast(bf16x8, u32x4{v, v, v, v});
+    };
+    auto use = [&](const Batch &b, int stage) __attribute__((always_inline)) {
+#pragma unroll
+        for (int g = 0; g < GPT; ++g) {
+            bf16x8 q[NW][MPG];
+            float s[NW];
+#pragma unroll
+            for (int w = 0; w < NW; ++w) {
+                s[w] = __builtin_bit_cast(float, Group::scale(b.s[w], g));
+#pragma unroll
+                for (int m = 0; m < MPG; ++m)
+                    q[w][m] = w4_unpack(b.w[w][g * MPG + m]);
+            }
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) {
+                bf16x8 x[MPG];
+#pragma unroll
+                for (int m = 0; m < MPG; ++m)
+                    x[m] = *(const bf16x8 *)(rows[stage] + nb * 16 * 256 + (x_read ^ (g * MPG + m) << 6));
+                f32x4 mid{};
+                if constexpr (!ZEROS)
+#pragma unroll
+                    for (int m = 0; m < MPG; ++m)
+                        mid = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[m], constant(kW4MinusMid), mid, 0, 0, 0);
+#pragma unroll
+                for (int w = 0; w < NW; ++w) {
+                    f32x4 acc = mid;
+                    if constexpr (ZEROS) {
+                        const uint32_t z = 0xbf80u | Group::zero(b.z[w], g); // -(1 + z / 128)
+#pragma unroll
+                        for (int m = 0; m < MPG; ++m)
+                            acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[m], constant(z | z << 16), acc, 0, 0, 0);
+                    }
+#pragma unroll
+                    for (int m = 0; m < MPG; ++m)
+                        acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[m], q[w][m], acc, 0, 0, 0);
+#pragma unroll
+                    for (int i = 0; i < 4; ++i)
+                        total[w][nb][i] += s[w] * acc[i];
+                }
+            }
+        }
+    };
+
+    // Step kt: the rows of kt + 1 go to the other stage, those of kt + 1 + XD and the
+    // weights of kt + DEPTH are asked for, kt is multiplied.  The barrier at its end
+    // (after this wave's LDS reads and writes) hands both stages over.
+    static_assert(DEPTH % XD == 0, "the rows' registers go round with the weights'");
+    Batch batch[DEPTH];
+    Rows ahead[XD];
+    {
+        Rows now;
+        load_rows(now, begin);
+#pragma unroll
+        for (int d = 0; d < XD; ++d)
+            load_rows(ahead[d], begin + 1 + d);
+#pragma unroll
+        for (int d = 0; d < DEPTH; ++d)
+            load(batch[d], begin + d);
+        store_rows(now, 0);
+    }
+    wait_lgkm0();
+    barrier_only();
+    auto step = [&](int kt, int d) __attribute__((always_inline)) {
+        const int stage = (kt - begin) & 1;
+        store_rows(ahead[d % XD], stage ^ 1);
+        load_rows(ahead[d % XD], kt + 1 + XD);
+        use(batch[d], stage);
+        load(batch[d], kt + DEPTH);
+        wait_lgkm0();
+        barrier_only();
+    };
+    int kt = begin;
+    for (; kt + DEPTH <= end; kt += DEPTH)
+#pragma unroll
+        for (int d = 0; d < DEPTH; ++d)
+            step(kt + d, d);
+#pragma unroll
+    for (int d = 0; d < DEPTH - 1; ++d)
+        if (kt + d < end)
+            step(kt + d, d);
+
+    // ---- the blocks over k, in order (as w4_kernel) --------------------------------
+    if (p.splits > 1) {
+        const __amdgpu_buffer_rsrc_t prs = make_rsrc(p.partial);
+        auto partial_at = [&](int sp, int w, int nb) __attribute__((always_inline)) {
+            return (uint32_t)((((sp * p.strips + strip) * kW4SharedWaves + wave) * NW + w) * NB + nb) * 1024u;
+        };
+#pragma unroll
+        for (int w = 0; w < NW; ++w)
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+                __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, total[w][nb]), prs, lane * 16,
+                                                       partial_at(split, w, nb), kCoherent);
+        wait_vmcnt<0>();
+        __syncthreads();
+        if (tid == 0) {
+            const uint32_t before =
+                __hip_atomic_fetch_add(p.counters + strip, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+            s_last = before == (uint32_t)(p.splits - 1);
+        }
+        __syncthreads();
+        if (!s_last)
+            return;
+        if (tid == 0)
+            __hip_atomic_store(p.counters + strip, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        for (int sp = 0; sp < p.splits; ++sp) {
+            f32x4 x[NW][NB];
+#pragma unroll
+            for (int w = 0; w < NW; ++w)
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb)
+                    x[w][nb] = __builtin_bit_cast(f32x4, __builtin_amdgcn_raw_buffer_load_b128(prs, lane * 16,
+                                                                                              partial_at(sp, w, nb), kCoherent));
+#pragma unroll
+            for (int w = 0; w < NW; ++w)
+#pragma unroll
+                for (int nb = 0; nb < NB; ++nb)
+                    total[w][nb] = sp == 0 ? x[w][nb] : total[w][nb] + x[w][nb];
+        }
+    }
+    const int n = column_tile * 16 + row;
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            const int t = 16 * nb + 4 * kq + i;
+            const float a = total[0][nb][i] * 128.0f, b = total[NW - 1][nb][i] * 128.0f; // (q - z) / 128 so far
+            if (t < p.T && n < p.N)
+                p.out[(size_t)t * p.N + n] =
+                    __builtin_bit_cast(uint16_t, (__bf16)(NW == 2 ? gate_act(a, p.activation, p.beta) * b : a));
+        }
+}
+
 // ---- laying out, rounding and restoring weights -----------------------------------
 
 struct W4LayoutParams {

@@ -66,11 +66,31 @@ def test_matmul(T, zeros, group):
         check("y", y, x.double() @ w, product_slack(x.double(), w, steps))
 
 
-@pytest.mark.parametrize("T,D,F", [(1, 264, 520), (3, 4096, 1024), (8, 520, 264), (30, 264, 1032), (64, 1032, 2056)])
+@pytest.mark.parametrize("group,zeros", [(64, False), (64, True), (128, False), (128, True)])
+@pytest.mark.parametrize("T,K,N", [(16, 2056, 12296), (33, 2056, 12296), (20, 6184, 4168), (48, 6184, 4168), (64, 6184, 4168)])
+def test_long_weights(T, K, N, group, zeros):
+    """The waves of a block share X: one block to a strip, and three over k (of 17, 17, 15 k-tiles)."""
+    print("w4 T=%d K=%d N=%d group=%d zeros=%s" % (T, K, N, group, zeros), flush=True)
+    gen = torch.Generator().manual_seed(T + K + N)
+    raw, w, steps = weight(K, N, group, zeros, gen)
+    x = torch.randn((T, K), generator=gen).to(torch.bfloat16)
+    p, ws = packed(raw, group), w4.make_workspace(T, K, N)
+    y = w4.matmul(x.cuda(), p, workspace=ws)
+    check("y", y, x.double() @ w, product_slack(x.double(), w, steps))
+    again = w4.matmul(x.cuda(), p)  # and without a workspace of its own
+    assert torch.equal(y, again)
+    # A row is its own, whatever is beside it.
+    other = torch.full_like(x, float("nan"))
+    other[T // 2] = x[T // 2]
+    assert torch.equal(w4.matmul(other.cuda(), p, workspace=ws)[T // 2], y[T // 2])
+
+
+@pytest.mark.parametrize("T,D,F", [(1, 264, 520), (3, 4096, 1024), (8, 520, 264), (30, 264, 1032), (64, 1032, 2056),
+                                   (17, 2056, 12296), (64, 12296, 2056)])
 @pytest.mark.parametrize("activation,beta", [("silu", 1.0), ("swish", 1.702), ("sigmoid", 1.0)])
 def test_forward(T, D, F, activation, beta):
     gen = torch.Generator().manual_seed(T + D)
-    zeros, group = T % 2 == 0, 128 if T < 8 else 32
+    zeros, group = T % 2 == 0, 128 if T < 8 else 64 if D * F > 2 ** 23 else 32
     (rg, wg, sg), (ru, wu, su), (rd, wd, sd) = (weight(K, N, group, zeros, gen) for K, N in ((D, F), (D, F), (F, D)))
     x = torch.randn((T, D), generator=gen).to(torch.bfloat16)
     pg, pu, pd = (packed(r, group) for r in (rg, ru, rd))

@@ -57,3 +57,9 @@ def test_layout_refusals():
     assert lib.gmlp_w4_quantize(at(0), at(2), None, None, 256, 512, 64, None) == 1
     assert lib.gmlp_w4_dequantize(at(0), at(0) + 1024, 256, 512, 64, 0, None) == 1
     assert lib.gmlp_w4_dequantize(at(0), None, 256, 512, 64, 0, None) == 1
+
+
+def test_a_workspace_serves_fewer_tokens():
+    for D, F in ((8, 8), (1024, 4096), (4168, 6184), (8192, 2048), (2056, 12296), (12296, 2056)):
+        sizes = [w4.workspace_size(T, D, F) for T in range(1, 65)]
+        assert sizes == sorted(sizes)
