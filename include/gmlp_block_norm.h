@@ -65,8 +65,9 @@ int gmlp_block_norm(const void *Y, const void *res, const void *w_pre, const voi
 
 /*
  * Bytes of workspace gmlp_block_norm_backward needs: fp32 partial sums of the
- * gradients of the gains and of a channel gate.  It needs no preparation.  0 if
- * the shape is invalid.
+ * gradients of the gains and of a channel gate.  Enough for fewer rows too.  It
+ * needs no preparation and is overwritten: memory that gmlp_workspace_init has
+ * prepared for other calls must be prepared again.  0 if the shape is invalid.
  */
 size_t gmlp_block_norm_workspace_size(int64_t T, int64_t D);
 

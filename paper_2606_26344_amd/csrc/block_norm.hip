@@ -136,7 +136,8 @@ int gmlp_block_norm(const void *Y, const void *res, const void *w_pre, const voi
     const bool rows = T > 0;
     const bool gate_rows = flags & GMLP_NORM_GATE_ROWS;
     if ((rc = check_norm_shape(T, D)) ||
-        (rows && (rc = check_norm_args(flags, res_scale, eps, Y, w_post, gate))) || (rc = check_ptr(Y, "Y", false)) || (rc = check_ptr(res, "res", rows)) || (rc = check_ptr(w_pre, "w_pre", false)) ||
+        (rows && (rc = check_norm_args(flags, res_scale, eps, Y, w_post, gate))) || (rc = check_ptr(Y, "Y", false)) ||
+        (rc = check_ptr(res, "res", rows)) || (rc = check_ptr(w_pre, "w_pre", false)) ||
         (rc = check_ptr(w_post, "w_post", false)) || (rc = check_ptr(gate, "gate", false)) ||
         (rc = check_ptr(R, "R", rows && Y)) || (rc = check_ptr(Xn, "Xn", rows)))
         return rc;
@@ -170,7 +171,8 @@ size_t gmlp_block_norm_workspace_size(int64_t T, int64_t D)
 {
     if (check_norm_shape(T, D))
         return 0;
-    return align_up((size_t)kNormSums * norm_backward_shape(T, D).blocks * D * sizeof(float));
+    // The most blocks that as many rows or fewer have: T + 1 rows may have fewer than T.
+    return align_up((size_t)kNormSums * std::min<int64_t>(std::max<int64_t>(T, 1), kBlockTarget) * D * sizeof(float));
 }
 
 int gmlp_block_norm_backward(const void *dXn, const void *dR, const void *Y, const void *R, const void *w_pre,
@@ -181,8 +183,8 @@ int gmlp_block_norm_backward(const void *dXn, const void *dR, const void *Y, con
     int rc;
     const bool rows = T > 0, gate_rows = flags & GMLP_NORM_GATE_ROWS;
     if ((rc = check_norm_shape(T, D)) ||
-        (rows && (rc = check_norm_args(flags, res_scale, eps, Y, w_post, gate))) || (rc = check_ptr(dXn, "dXn", rows)) || (rc = check_ptr(dR, "dR", false)) || (rc = check_ptr(Y, "Y", false)) ||
-        (rc = check_ptr(R, "R", rows)) || (rc = check_ptr(w_pre, "w_pre", false)) ||
+        (rows && (rc = check_norm_args(flags, res_scale, eps, Y, w_post, gate))) || (rc = check_ptr(dXn, "dXn", rows)) ||
+        (rc = check_ptr(dR, "dR", false)) || (rc = check_ptr(Y, "Y", false)) || (rc = check_ptr(R, "R", rows)) || (rc = check_ptr(w_pre, "w_pre", false)) ||
         (rc = check_ptr(w_post, "w_post", false)) || (rc = check_ptr(gate, "gate", false)) ||
         (rc = check_ptr(dY, "dY", false)) || (rc = check_ptr(dres, "dres", false)) ||
         (rc = check_ptr(dw_pre, "dw_pre", false)) || (rc = check_ptr(dw_post, "dw_post", false)) ||

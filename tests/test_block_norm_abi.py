@@ -62,3 +62,8 @@ def test_no_rows_launches_nothing_where_nothing_is_wanted():
 def test_workspace_size():
     assert block_norm.workspace_size(0, 8) > 0 and block_norm.workspace_size(4096, 4096) >= 3 * 4096 * 4
     assert block_norm.workspace_size(4, 12) == 0 and block_norm.workspace_size(-1, 8) == 0
+    for D in (8, 520, 2048, 4096, 16384):
+        sizes = [block_norm.workspace_size(T, D) for T in range(0, 1200)]
+        assert sizes == sorted(sizes)  # one made for many rows serves fewer
+        for T in (1 << 14, 1 << 23):
+            assert block_norm.workspace_size(T, D) == sizes[-1]
