@@ -3,6 +3,8 @@
 // with no HIP dependency.
 #pragma once
 
+#include <cmath>
+
 #include "plan.hpp"
 
 namespace gmlp {
@@ -150,19 +152,26 @@ constexpr bool grad_tile_fits(GradTile t, bool weight)
     return t == GRAD_LARGE || t == GRAD_SMALL || (t == GRAD_PAIR) == weight;
 }
 
-// The tile with the least estimated time.
+// The tile with the least estimated time.  Its rows of the widest tensor are addressed
+// with 31 bits from its corner: only the tiles of up to 192 lines take every width.
 inline GradStep grad_step(int problems, int64_t M, int64_t N, int64_t K, int segments, bool weight)
 {
     GradStep best;
     double best_time = 0.0;
+    bool found = false;
+    const int64_t widest = weight ? std::max(M, N) : std::max(M, K);
     for (int t = 0; t < GRAD_TILES; ++t) {
         if (!grad_tile_fits((GradTile)t, weight))
             continue;
         GradStep s;
         const double time = with_grad_tile((GradTile)t, [&](auto tag) {
-            return grad_candidate<typename decltype(tag)::type>(s, (GradTile)t, problems, M, N, K, segments);
+            using S = typename decltype(tag)::type;
+            return std::max(S::BM, S::BN) * widest * 2 >= (int64_t(1) << 31)
+                       ? HUGE_VAL
+                       : grad_candidate<S>(s, (GradTile)t, problems, M, N, K, segments);
         });
-        if (t == 0 || time < best_time) {
+        if (time < HUGE_VAL && (!found || time < best_time)) {
+            found = true;
             best = s;
             best_time = time;
         }
@@ -191,7 +200,8 @@ inline Step train_gate_up_step(int64_t T, int64_t D, int64_t F)
 {
     Step s;
     const int64_t large_tiles = cdiv(T, GateUpLarge::BN) * cdiv(F, GateUpLarge::BMW);
-    if (large_tiles >= 512 || (T > 256 && large_tiles >= 192))
+    const bool large = F < kMaxDim; // H, G and U of 256 tokens from the tile's corner in 31 bits
+    if (large && (large_tiles >= 512 || (T > 256 && large_tiles >= 192)))
         gemm_step<GateUpLarge>(s, K_GEMM_GU_L, (int)F, (int)T, (int)D, 2, false, kGroupGateUp);
     else if (T <= GateUpTiny::BN)
         gemm_step<GateUpTiny>(s, K_GEMM_GU_T, (int)F, (int)T, (int)D, 2, true, kGroupGateUp);

@@ -129,6 +129,44 @@ def test_tiles(T, D, F, dh, dx, dw):
     run(T, D, F, seed=3)
 
 
+@pytest.mark.parametrize("T", [1, 256])
+def test_widest_tensors(T):
+    """F = 2^22: the last of 256 rows ends 2 GiB after the first begins.
+
+    dX sums 2^23 products, in fp32 in 85 (T = 1: more) pieces of MFMA steps of 32: (2^23 /
+    85 / 32 + 32 + 256) 2^-24 < 2^-12 of its terms, as above."""
+    D, F = 8, 1 << 22
+    print("train T=%d D=%d F=%d" % (T, D, F), flush=True)
+    gen = torch.Generator(device="cuda").manual_seed(T)
+    n = lambda r, c, s: (torch.randn((r, c), generator=gen, device="cuda") * s).to(torch.bfloat16)  # noqa: E731
+    x, wg, wu, wd, dy = n(T, D, 1.0), n(D, F, D ** -0.5), n(D, F, D ** -0.5), n(F, D, F ** -0.5), n(T, D, 1.0)
+    ws = train.make_workspace(T, D, F)
+    y, g, u = train.forward(x, wg, wu, wd, workspace=ws)
+    dx, dwg, dwu, dwd = train.backward(dy, x, wg, wu, wd, g, u, workspace=ws)
+    xd, dyd = x.double(), dy.double()
+    total = torch.zeros((3, T, D), dtype=torch.float64, device="cuda")
+    step = 1 << 18
+    for c in range(0, F, step):
+        cols = slice(c, c + step)
+        wgd, wud, wdd = wg[:, cols].double(), wu[:, cols].double(), wd[cols].double()
+        gd, ud = g[:, cols].double(), u[:, cols].double()
+        assert ((gd - xd @ wgd).abs() <= HALF_STEP * gd.abs() * 1.01 + 2.0 ** -12 * (xd.abs() @ wgd.abs())).all(), c
+        assert ((ud - xd @ wud).abs() <= HALF_STEP * ud.abs() * 1.01 + 2.0 ** -12 * (xd.abs() @ wud.abs())).all(), c
+        a, da = act(gd, "silu", 1.0)
+        dh, dht = dyd @ wdd.T, dyd.abs() @ wdd.abs().T
+        dg, du, h = dh * ud * da, dh * a, a * ud
+        dgt, dut = dg.abs() + 2.0 ** -4 * (dht * ud * da).abs(), du.abs() + 2.0 ** -4 * (dht * a).abs()
+        total[0] += dg @ wgd.T + du @ wud.T
+        total[1] += dgt @ wgd.abs().T + dut @ wud.abs().T
+        total[2] += h @ wdd
+        for name, got, ref, terms in (("dwg", dwg[:, cols], xd.T @ dg, xd.abs().T @ dgt),
+                                      ("dwu", dwu[:, cols], xd.T @ du, xd.abs().T @ dut),
+                                      ("dwd", dwd[cols], h.T @ dyd, h.abs().T @ dyd.abs())):
+            bound = HALF_STEP * ref.abs() + ROUNDED * terms + 1e-30
+            assert ((got.double() - ref).abs() <= bound).all(), (name, c)
+    check("dx", dx, total[0], total[1])
+
+
 @pytest.mark.parametrize("want", [("dx",), ("dwd",), ("dwg", "dwu"), ("dx", "dwu"), ()])
 def test_wanted_gradients_only(want):
     run(70, 264, 520, want=want, seed=9)

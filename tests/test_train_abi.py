@@ -62,3 +62,15 @@ def test_workspace_and_plans():
             assert grid * block < 1 << 32 and splits >= 1
     assert [k[0].split("<")[0] for k in train.describe(300, 1032, 2056, False)] == ["gemm_mfma_kernel"] * 2
     assert len(train.describe(300, 1032, 2056)) == 3 and len(train.describe(0, 8, 8)) == 1
+
+
+def test_tiles_of_the_widest_tensors():
+    """A tile's rows are addressed with 31 bits: fewer than 256 of a width of 2^22."""
+    for D, F in ((8, 1 << 22), (1 << 22, 8), (256, 1 << 22)):
+        for T in (1, 64, 257, 512, 4096):
+            kernels = train.describe(T, D, F) + (train.describe(T, D, F, backward=False)[:1] if F > D else [])
+            for name, *_ in kernels:
+                wm, wn, tm, tn = (int(v) for v in name.split("Shape<")[1].split(",")[:4])
+                if "Grad" in name:
+                    assert max(wm * tm, wn * tn) * 32 < 256, (T, D, F, name)
+    assert any("<4, 2, 2, 4" in k[0] for k in train.describe(4096, 4096, 1 << 21))
