@@ -21,7 +21,7 @@ from typing import Optional
 
 import torch
 
-from .gmlp import _CALL_DEVICE, _check, _empty, _empty_like, _expect, _ptr, _scratch, _stream, library
+from .gmlp import _CALL_DEVICE, _check, _empty, _empty_like, _expect, _on_current, _ptr, _scratch, _stream, library
 
 POST, RES_FP32, GATE_ROWS = 1, 2, 4
 
@@ -31,7 +31,9 @@ def workspace_size(T: int, D: int) -> int:
 
 
 class Workspace:
-    """A caller-owned workspace for backward(); it needs no preparation."""
+    """A caller-owned workspace for backward(); it needs no preparation.  (The
+    calls of the other modules need theirs prepared, which backward() would undo:
+    neither takes the other's.)"""
 
     def __init__(self, T: int, D: int, device=None, stream=None):
         n = workspace_size(T, D)
@@ -68,6 +70,7 @@ def _options(like, name, w_pre, w_post, gate, post):
     dev = like.device
     if dev.type != "cuda":
         raise ValueError("%s must be on a HIP device, got %s" % (name, dev))
+    _on_current(dev)
     _stream_tensor(like, name, (T, D), dev, like.dtype)
     flags = (POST if post else 0) | (RES_FP32 if like.dtype is torch.float32 else 0)
     for t, n in ((w_pre, "w_pre"), (w_post, "w_post")):
@@ -134,6 +137,10 @@ def backward(dxn: torch.Tensor, dr: Optional[torch.Tensor], y: Optional[torch.Te
     if workspace is None:
         nbytes = workspace_size(T, D)
         keep, ws = _scratch(nbytes, 1, _CALL_DEVICE, stream, False, "invalid shape T=%d D=%d" % (T, D))
+    elif not isinstance(workspace, Workspace):
+        raise TypeError("workspace must be one of make_workspace(), got %s" % type(workspace).__name__)
+    elif workspace.buffer.device != dev:
+        raise ValueError("workspace must be on %s, got %s" % (dev, workspace.buffer.device))
     else:
         keep, ws, nbytes = None, workspace.buffer.data_ptr(), workspace.nbytes
     _check(library().gmlp_block_norm_backward(

@@ -226,6 +226,22 @@ def _expect(t: torch.Tensor, name: str, shape, device) -> None:
         raise ValueError("%s has shape %s, expected %s" % (name, tuple(t.shape), tuple(shape)))
 
 
+def _on_current(device) -> None:
+    """Refuses tensors of another device than the current one, on which the
+    library launches and takes memory."""
+    if device.index != torch._C._cuda_getDevice():
+        raise ValueError("the tensors are on %s, the current device is cuda:%d" % (device, torch._C._cuda_getDevice()))
+
+
+def _prepared(workspace, device):
+    """(address, bytes) of a Workspace whose counters are prepared."""
+    if not isinstance(workspace, Workspace):
+        raise TypeError("workspace must be one of make_workspace(), got %s" % type(workspace).__name__)
+    if workspace.buffer.device != device:
+        raise ValueError("workspace must be on %s, got %s" % (device, workspace.buffer.device))
+    return workspace.buffer.data_ptr(), workspace.nbytes
+
+
 def describe(T: int, D: int, F: int, path: str = "auto") -> list:
     """The kernels forward() enqueues for this shape: a list of
     (name, grid, block, k_splits), in launch order."""

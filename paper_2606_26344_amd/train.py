@@ -20,8 +20,8 @@ from typing import Optional, Sequence
 
 import torch
 
-from .gmlp import (_CALL_DEVICE, FRESH_WORKSPACE, PATH_AUTO, Workspace, _check, _empty, _empty_like, _expect, _parse_plan, _ptr,
-                   _scratch, _stream, _variant, library)
+from .gmlp import (_CALL_DEVICE, FRESH_WORKSPACE, PATH_AUTO, Workspace, _check, _empty, _empty_like, _expect,
+                   _on_current, _parse_plan, _prepared, _ptr, _scratch, _stream, _variant, library)
 
 GRADIENTS = ("dx", "dwg", "dwu", "dwd")
 
@@ -45,10 +45,10 @@ def describe(T: int, D: int, F: int, backward: bool = True) -> list:
     return _parse_plan(buf)
 
 
-def _workspace(workspace, T, D, F, rows, stream):
+def _workspace(workspace, T, D, F, device, rows, stream):
     """(tensor to keep, address, bytes, path) of a call's workspace."""
     if workspace is not None:
-        return None, workspace.buffer.data_ptr(), workspace.nbytes, PATH_AUTO
+        return None, *_prepared(workspace, device), PATH_AUTO
     n = workspace_size(T, D, F)
     keep, ws = _scratch(n, rows, _CALL_DEVICE, stream, False, "invalid shape T=%d D=%d F=%d" % (T, D, F))
     return keep, ws, n, PATH_AUTO | FRESH_WORKSPACE
@@ -72,6 +72,7 @@ def _weights(x, wg, wu, wd):
     _expect(wg, "wg", (D, F), dev)
     _expect(wu, "wu", (D, F), dev)
     _expect(wd, "wd", (F, D), dev)
+    _on_current(dev)
     return T, D, F, dev
 
 
@@ -87,7 +88,7 @@ def forward(x: torch.Tensor, wg: torch.Tensor, wu: torch.Tensor, wd: torch.Tenso
     u = _empty_like(g, stream) if u is None else u
     _expect(g, "g", (T, F), dev)
     _expect(u, "u", (T, F), dev)
-    keep, ws, nbytes, path = _workspace(workspace, T, D, F, T, stream)
+    keep, ws, nbytes, path = _workspace(workspace, T, D, F, dev, T, stream)
     _check(library().gmlp_train_forward(x.data_ptr(), wg.data_ptr(), wu.data_ptr(), wd.data_ptr(), out.data_ptr(),
                                         g.data_ptr(), u.data_ptr(), T, D, F, act, beta, path, ws, nbytes,
                                         _stream(stream)))
@@ -119,7 +120,7 @@ def backward(dy: torch.Tensor, x: torch.Tensor, wg: torch.Tensor, wu: torch.Tens
         else:
             outs.append(None)
     # The weight gradients of no tokens are zeros, which a kernel writes.
-    keep, ws, nbytes, path = _workspace(workspace, T, D, F, 1, stream)
+    keep, ws, nbytes, path = _workspace(workspace, T, D, F, dev, 1, stream)
     _check(library().gmlp_train_backward(dy.data_ptr(), x.data_ptr(), wg.data_ptr(), wu.data_ptr(), wd.data_ptr(),
                                          g.data_ptr(), u.data_ptr(), *[_ptr(t) for t in outs], T, D, F, act, beta,
                                          path, ws, nbytes, _stream(stream)))

@@ -21,8 +21,8 @@ from typing import Optional
 
 import torch
 
-from .gmlp import (_CALL_DEVICE, FRESH_WORKSPACE, PATH_AUTO, Workspace, _check, _empty, _expect, _ptr, _scratch,
-                   _stream, _variant, library)
+from .gmlp import (_CALL_DEVICE, FRESH_WORKSPACE, PATH_AUTO, Workspace, _check, _empty, _expect, _on_current, _prepared,
+                   _ptr, _scratch, _stream, _variant, library)
 
 MAX_TOKENS = 64
 
@@ -68,6 +68,7 @@ def quantize(w: torch.Tensor, group: int = 128, zeros: bool = False, stream=None
     K, N = w.shape
     dev = w.device
     _expect(w, "w", (K, N), dev)
+    _on_current(dev)
     groups = -(-K // max(group, 1))
     q = _empty((K, N), torch.uint8, dev, stream)
     s = _empty((groups, N), torch.bfloat16, dev, stream)
@@ -85,6 +86,7 @@ def pack(q: torch.Tensor, scales: torch.Tensor, zeros: Optional[torch.Tensor] = 
     dev = q.device
     if dev.type != "cuda":
         raise ValueError("q must be on a HIP device, got %s" % dev)
+    _on_current(dev)
     shape = (-(-K // max(group, 1)), N)
     _expect_bytes(q, "q", (K, N), dev)
     _expect(scales, "scales", shape, dev)
@@ -104,6 +106,7 @@ def from_weight(w: torch.Tensor, group: int = 128, zeros: bool = False, stream=N
 def dequantize(w: Weight, out: Optional[torch.Tensor] = None, stream=None) -> torch.Tensor:
     """bf16((q - zeros) * scales) [K, N], for example for the entry points of
     :mod:`paper_2606_26344_amd.gmlp` with many tokens."""
+    _on_current(w.device)
     if out is None:
         out = _empty((w.K, w.N), torch.bfloat16, w.device, stream)
     else:
@@ -113,10 +116,10 @@ def dequantize(w: Weight, out: Optional[torch.Tensor] = None, stream=None) -> to
     return out
 
 
-def _workspace(workspace, T, D, F, stream):
+def _workspace(workspace, T, D, F, device, stream):
     """(tensor to keep, address, bytes, path) of a call's workspace."""
     if workspace is not None:
-        return None, workspace.buffer.data_ptr(), workspace.nbytes, PATH_AUTO
+        return None, *_prepared(workspace, device), PATH_AUTO
     n = workspace_size(T, D, F)
     if n == 0 and T > MAX_TOKENS:  # refused by the library, with its reason
         return None, None, 0, PATH_AUTO
@@ -144,6 +147,7 @@ def _first(x, w, name):
     T, dev = x.shape[0], x.device
     _expect(x, "x", (T, w.K), dev)
     _expect_weight(w, name, w.K, w.N, w, dev)
+    _on_current(dev)
     return T, dev
 
 
@@ -159,7 +163,7 @@ def matmul(x: torch.Tensor, w: Weight, out: Optional[torch.Tensor] = None, works
     """y = x w, x [T, K]."""
     T, dev = _first(x, w, "w")
     out = _output(out, T, w.N, dev, stream)
-    keep, ws, nbytes, path = _workspace(workspace, T, w.K, w.N, stream)
+    keep, ws, nbytes, path = _workspace(workspace, T, w.K, w.N, dev, stream)
     _check(library().gmlp_w4_matmul(x.data_ptr(), w.buffer.data_ptr(), out.data_ptr(), T, w.K, w.N, w.group,
                                     int(w.zeros), path, ws, nbytes, _stream(stream)))
     return out
@@ -172,7 +176,7 @@ def gate_up(x: torch.Tensor, wg: Weight, wu: Weight, out: Optional[torch.Tensor]
     _expect_weight(wu, "wu", wg.K, wg.N, wg, dev)
     act, beta, _, _ = _variant(activation, beta, False, 0.0)
     out = _output(out, T, wg.N, dev, stream)
-    keep, ws, nbytes, path = _workspace(workspace, T, wg.K, wg.N, stream)
+    keep, ws, nbytes, path = _workspace(workspace, T, wg.K, wg.N, dev, stream)
     _check(library().gmlp_w4_gate_up(x.data_ptr(), wg.buffer.data_ptr(), wu.buffer.data_ptr(), out.data_ptr(), T, wg.K,
                                      wg.N, wg.group, int(wg.zeros), act, beta, path, ws, nbytes, _stream(stream)))
     return out
@@ -188,7 +192,7 @@ def forward(x: torch.Tensor, wg: Weight, wu: Weight, wd: Weight, out: Optional[t
     _expect_weight(wd, "wd", F, D, wg, dev)
     act, beta, _, _ = _variant(activation, beta, False, 0.0)
     out = _output(out, T, D, dev, stream)
-    keep, ws, nbytes, path = _workspace(workspace, T, D, F, stream)
+    keep, ws, nbytes, path = _workspace(workspace, T, D, F, dev, stream)
     _check(library().gmlp_w4_forward(x.data_ptr(), wg.buffer.data_ptr(), wu.buffer.data_ptr(), wd.buffer.data_ptr(),
                                      out.data_ptr(), T, D, F, wg.group, int(wg.zeros), act, beta, path, ws, nbytes,
                                      _stream(stream)))
