@@ -194,21 +194,16 @@ inline GradPlan grad_plan(int64_t T, int64_t D, int64_t F)
 // The weight gradients, as many as are wanted.
 inline GradStep grad_weight_step(int problems, int64_t T, int64_t D, int64_t F) { return grad_step(problems, F, D, T, 1, true); }
 
-// The gate/up step of the training forward pass: the tiles of make_plan that
-// cover every token count, with H, G and U in the epilogue.
+// The gate/up step of the training forward pass: the forward pass's tiles that hold
+// both weights, with H, G and U in the epilogue.
 inline Step train_gate_up_step(int64_t T, int64_t D, int64_t F)
 {
-    Step s;
-    const int64_t large_tiles = cdiv(T, GateUpLarge::BN) * cdiv(F, GateUpLarge::BMW);
-    const bool large = F < kMaxDim; // H, G and U of 256 tokens from the tile's corner in 31 bits
-    if (large && (large_tiles >= 512 || (T > 256 && large_tiles >= 192)))
-        gemm_step<GateUpLarge>(s, K_GEMM_GU_L, (int)F, (int)T, (int)D, 2, false, kGroupGateUp);
-    else if (T <= GateUpTiny::BN)
-        gemm_step<GateUpTiny>(s, K_GEMM_GU_T, (int)F, (int)T, (int)D, 2, true, kGroupGateUp);
-    else if (T <= GateUpMid::BN)
-        gemm_step<GateUpMid>(s, K_GEMM_GU_M, (int)F, (int)T, (int)D, 2, true, kGroupGateUp);
-    else
+    Step s = gate_up_tiles(T, D, F);
+    // H, G and U of 256 tokens from the tile's corner in 31 bits.
+    if (s.kind == K_GEMM_GU_L && F == kMaxDim) {
+        s = Step{};
         gemm_step<GateUpSmall>(s, K_GEMM_GU_S, (int)F, (int)T, (int)D, 2, true, kGroupGateUp);
+    }
     return s;
 }
 

@@ -591,6 +591,49 @@ inline void gemv_step(Step &s, int M, int N, int K, int nw)
     s.partial_bytes = s.splits > 1 ? (size_t)s.splits * ((size_t)nw * N * M + (size_t)s.strips * N) * sizeof(float) : 0;
 }
 
+// The gate/up step's tiles whose blocks hold both weights.
+inline Step gate_up_tiles(int64_t T, int64_t D, int64_t F)
+{
+    Step s;
+    // Large tiles once there are enough of them to fill the chip,
+    // and above 256 tokens once they at least nearly fill it: there one
+    // round of large tiles beats the partial second round that small tiles
+    // leave (measured at D = 4096, F = 14336: T = 320, 384 11% faster,
+    // T = 512 and 1024 8%).
+    const int64_t large_tiles = cdiv(T, GateUpLarge::BN) * cdiv(F, GateUpLarge::BMW);
+    // Two 192-token tiles where they make one round that is at least three
+    // quarters full (measured at D = 4096, F = 14336 against two 256-token
+    // tiles, gate/up: T = 257 111.8 -> 89.0 us, 320 114.2 -> 93.5, 384
+    // 115.8 -> 98.3; 8 waves with 64-row k-tiles were 6-11% slower).
+    const int64_t tiles192 = cdiv(T, GateUp192::BN) * cdiv(F, GateUp192::BMW);
+    // 129 to 256 tokens with 129 to 256 column tiles, where two 128-token
+    // tiles of each would take a second round: one 192- or 256-token tile
+    // instead, in one round, each weight element read once (the weights
+    // streamed).  Measured, gate/up: D = 8192, F = 28672 T = 129 311.8 -> 199.0 us,
+    // 192 308.9 -> 198.6, 256 318.0 -> 240.6; D = 4400, F = 16648 (131 tiles) T = 129
+    // 135.8 -> 101.4, 193 143.8 -> 124.5; D = 4096, F = 20480 T = 160 129.9 -> 98.2,
+    // 256 139.6 -> 116.3.
+    const int64_t columns = cdiv(F, GateUpLarge::BMW);
+    const bool one_round = columns > kBlockTarget / 2 && columns <= kBlockTarget;
+    if (T > GateUpSmall::BN && T <= GateUp192::BN && one_round)
+        gemm_step<GateUp192>(s, K_GEMM_GU_Y, (int)F, (int)T, (int)D, 2, false, kGroupGateUp);
+    else if (T > GateUp192::BN && T <= 256 && one_round)
+        gemm_step<GateUpLarge>(s, K_GEMM_GU_L, (int)F, (int)T, (int)D, 2, false, kGroupGateUp);
+    else if (T > 256 && T <= 2 * GateUp192::BN && tiles192 <= kBlockTarget && tiles192 >= kBlockTarget * 3 / 4)
+        gemm_step<GateUp192>(s, K_GEMM_GU_Y, (int)F, (int)T, (int)D, 2, false, kGroupGateUp);
+    else if (large_tiles >= 512 || (T > 256 && large_tiles >= 192))
+        gemm_step<GateUpLarge>(s, K_GEMM_GU_L, (int)F, (int)T, (int)D, 2, false, kGroupGateUp);
+    else if (T <= GateUpTiny::BN)
+        gemm_step<GateUpTiny>(s, K_GEMM_GU_T, (int)F, (int)T, (int)D, 2, true, kGroupGateUp);
+    else if (T <= GateUpMid::BN)
+        gemm_step<GateUpMid>(s, K_GEMM_GU_M, (int)F, (int)T, (int)D, 2, true, kGroupGateUp);
+    else if (T <= GateUpMid96::BN)
+        gemm_step<GateUpMid96>(s, K_GEMM_GU_W, (int)F, (int)T, (int)D, 2, true, kGroupGateUp);
+    else
+        gemm_step<GateUpSmall>(s, K_GEMM_GU_S, (int)F, (int)T, (int)D, 2, true, kGroupGateUp);
+    return s;
+}
+
 inline Plan make_plan(int64_t T, int64_t D, int64_t F, int path)
 {
     Plan p;
@@ -627,42 +670,7 @@ inline Plan make_plan(int64_t T, int64_t D, int64_t F, int path)
         }
         return p;
     }
-    // Gate/up: large tiles once there are enough of them to fill the chip,
-    // and above 256 tokens once they at least nearly fill it: there one
-    // round of large tiles beats the partial second round that small tiles
-    // leave (measured at D = 4096, F = 14336: T = 320, 384 11% faster,
-    // T = 512 and 1024 8%).
-    const int64_t large_tiles = cdiv(T, GateUpLarge::BN) * cdiv(F, GateUpLarge::BMW);
-    // Two 192-token tiles where they make one round that is at least three
-    // quarters full (measured at D = 4096, F = 14336 against two 256-token
-    // tiles, gate/up: T = 257 111.8 -> 89.0 us, 320 114.2 -> 93.5, 384
-    // 115.8 -> 98.3; 8 waves with 64-row k-tiles were 6-11% slower).
-    const int64_t tiles192 = cdiv(T, GateUp192::BN) * cdiv(F, GateUp192::BMW);
-    // 129 to 256 tokens with 129 to 256 column tiles, where two 128-token
-    // tiles of each would take a second round: one 192- or 256-token tile
-    // instead, in one round, each weight element read once (the weights
-    // streamed).  Measured, gate/up: D = 8192, F = 28672 T = 129 311.8 -> 199.0 us,
-    // 192 308.9 -> 198.6, 256 318.0 -> 240.6; D = 4400, F = 16648 (131 tiles) T = 129
-    // 135.8 -> 101.4, 193 143.8 -> 124.5; D = 4096, F = 20480 T = 160 129.9 -> 98.2,
-    // 256 139.6 -> 116.3.
-    const int64_t columns = cdiv(F, GateUpLarge::BMW);
-    const bool one_round = columns > kBlockTarget / 2 && columns <= kBlockTarget;
-    if (T > GateUpSmall::BN && T <= GateUp192::BN && one_round)
-        gemm_step<GateUp192>(p.gate_up, K_GEMM_GU_Y, (int)F, (int)T, (int)D, 2, false, kGroupGateUp);
-    else if (T > GateUp192::BN && T <= 256 && one_round)
-        gemm_step<GateUpLarge>(p.gate_up, K_GEMM_GU_L, (int)F, (int)T, (int)D, 2, false, kGroupGateUp);
-    else if (T > 256 && T <= 2 * GateUp192::BN && tiles192 <= kBlockTarget && tiles192 >= kBlockTarget * 3 / 4)
-        gemm_step<GateUp192>(p.gate_up, K_GEMM_GU_Y, (int)F, (int)T, (int)D, 2, false, kGroupGateUp);
-    else if (large_tiles >= 512 || (T > 256 && large_tiles >= 192))
-        gemm_step<GateUpLarge>(p.gate_up, K_GEMM_GU_L, (int)F, (int)T, (int)D, 2, false, kGroupGateUp);
-    else if (T <= GateUpTiny::BN)
-        gemm_step<GateUpTiny>(p.gate_up, K_GEMM_GU_T, (int)F, (int)T, (int)D, 2, true, kGroupGateUp);
-    else if (T <= GateUpMid::BN)
-        gemm_step<GateUpMid>(p.gate_up, K_GEMM_GU_M, (int)F, (int)T, (int)D, 2, true, kGroupGateUp);
-    else if (T <= GateUpMid96::BN)
-        gemm_step<GateUpMid96>(p.gate_up, K_GEMM_GU_W, (int)F, (int)T, (int)D, 2, true, kGroupGateUp);
-    else
-        gemm_step<GateUpSmall>(p.gate_up, K_GEMM_GU_S, (int)F, (int)T, (int)D, 2, true, kGroupGateUp);
+    p.gate_up = gate_up_tiles(T, D, F);
     if ((p.gate_up.kind == K_GEMM_GU_W || p.gate_up.kind == K_GEMM_GU_S) && p.gate_up.tiles_n == 1 &&
         p.gate_up.splits == 2 && p.gate_up.blocks >= kPairMinBlocks) {
         if (T <= PairMid96::BN)

@@ -89,13 +89,23 @@ int launch_save(const Step &s, const void *X, const void *Wg, const void *Wu, vo
 int run_save(const Step &s, const void *X, const void *Wg, const void *Wu, void *H, void *G, void *U, uint8_t *ws,
              const Layout &l, const Variant &v, hipStream_t st)
 {
+    // The weights are streamed where every element is read once.
+    const bool stream = stream_weights(s);
     switch (s.kind) {
     case K_GEMM_GU_L:
-        return s.tail_tiles ? launch_save<GateUpLarge, true, false>(tail_step(s), X, Wg, Wu, H, G, U, ws, l, v, st, s.tile_count)
-                            : launch_save<GateUpLarge, false, false>(s, X, Wg, Wu, H, G, U, ws, l, v, st);
-    case K_GEMM_GU_S: return launch_save<GateUpSmall, true, false>(s, X, Wg, Wu, H, G, U, ws, l, v, st);
+        if (s.tail_tiles)
+            return launch_save<GateUpLarge, true, false>(tail_step(s), X, Wg, Wu, H, G, U, ws, l, v, st, s.tile_count);
+        return stream ? launch_save<GateUpLarge, false, true>(s, X, Wg, Wu, H, G, U, ws, l, v, st)
+                      : launch_save<GateUpLarge, false, false>(s, X, Wg, Wu, H, G, U, ws, l, v, st);
+    case K_GEMM_GU_Y:
+        return stream ? launch_save<GateUp192, false, true>(s, X, Wg, Wu, H, G, U, ws, l, v, st)
+                      : launch_save<GateUp192, false, false>(s, X, Wg, Wu, H, G, U, ws, l, v, st);
+    case K_GEMM_GU_S:
+        return stream ? launch_save<GateUpSmall, true, true>(s, X, Wg, Wu, H, G, U, ws, l, v, st)
+                      : launch_save<GateUpSmall, true, false>(s, X, Wg, Wu, H, G, U, ws, l, v, st);
     case K_GEMM_GU_T: return launch_save<GateUpTiny, true, true>(s, X, Wg, Wu, H, G, U, ws, l, v, st);
     case K_GEMM_GU_M: return launch_save<GateUpMid, true, true>(s, X, Wg, Wu, H, G, U, ws, l, v, st);
+    case K_GEMM_GU_W: return launch_save<GateUpMid96, true, true>(s, X, Wg, Wu, H, G, U, ws, l, v, st);
     default: return fail(GMLP_ERR_INVALID_ARG, "internal: no gate/up kernel for this plan");
     }
 }
@@ -166,11 +176,6 @@ int gmlp_train_describe(int64_t T, int64_t D, int64_t F, int backward, char *buf
         const size_t at = text.find(", 0, ", text.find('>'));
         if (at != std::string::npos)
             text[at + 2] = '3'; // the epilogue that saves G and U
-        if (s.kind == K_GEMM_GU_S || (s.kind == K_GEMM_GU_L && !s.tail_tiles)) {
-            const size_t w = text.find(", true> grid"); // these never stream the weights
-            if (w != std::string::npos)
-                text.replace(w, 7, ", false>");
-        }
         text += describe_step(make_plan(T, D, F, GMLP_PATH_AUTO).down, false);
     }
     snprintf(buf, bytes, "%s", text.c_str());

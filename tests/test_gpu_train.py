@@ -129,6 +129,22 @@ def test_tiles(T, D, F, dh, dx, dw):
     run(T, D, F, seed=3)
 
 
+# (T, D, F, tile of the forward pass, streamed weights).
+FORWARD_TILES = [(20, 264, 520, "2, 4, 1, 1, 1, 4, 64", True), (50, 264, 520, "2, 4, 1, 1, 2, 3, 64", True),
+                 (90, 264, 520, "2, 4, 1, 1, 3, 3, 64", True),
+                 (100, 264, 520, "2, 4, 2, 1, 2, 3, 64", True), (150, 264, 16648, "2, 4, 1, 1, 6, 4, 32", True),
+                 (250, 264, 16648, "2, 4, 2, 1, 4, 2, 64", True), (300, 264, 12296, "2, 4, 1, 1, 6, 4, 32", False),
+                 (500, 136, 16392, "2, 4, 2, 1, 4, 2, 64", False), (300, 264, 520, "2, 4, 2, 1, 2, 3, 64", False)]
+
+
+@pytest.mark.parametrize("T,D,F,tile,stream", FORWARD_TILES, ids=["T%dD%dF%d" % c[:3] for c in FORWARD_TILES])
+def test_forward_tiles(T, D, F, tile, stream):
+    name = train.describe(T, D, F, backward=False)[0][0]
+    assert tile is None or "<%s>, 3" % tile in name, name
+    assert name.endswith("true>" if stream else "false>"), name
+    run(T, D, F, seed=5, want=())
+
+
 @pytest.mark.parametrize("T", [1, 256])
 def test_widest_tensors(T):
     """F = 2^22: the last of 256 rows ends 2 GiB after the first begins.
