@@ -34,19 +34,24 @@ namespace {
 
 // Tiles of the gradient matmuls.  The tall ones are for the products with a
 // weight (dH, dX) of few tokens: 128 rows of the weight against all the tokens, so
-// that each weight element is staged once.  The pair is for weight gradients of few
-// tokens: the stores and first loads of one block go on beside the MFMAs of the
-// other.  Measured, us, dH and dX for each tile and dW (D = 4096, F = 14336; in
-// brackets D = 5120, F = 13824):
+// that each weight element is staged once.  The pair and the short tile are for weight
+// gradients of few tokens: the stores and first loads of one block go on beside the
+// MFMAs of the other.  Measured, us, dH and dX for each tile and dW (D = 4096, F = 14336;
+// in brackets D = 5120, F = 13824):
 //   dH + dX  T = 16    128 x 32 83, 64 86, 128 89, 192 96, 320 111, 256 x 256 112
 //            T = 64    128 x 64 95, 32 108 (dX), 128 100, 256 x 256 147 (dX)
 //            T = 300   [dX: 128 x 160 104, 320 107, 128 107, 256 x 256 129]
-//   dW       T = 16    256 x 256 103, pair 90, 128 x 128 158
-//            T = 300   [200, 173, 284]
-//            T = 600   263, 244, 344
-//            T = 4096  1100, 1190, 1500
+//   dW       T = 30    short 90, pair 117
+//            T = 80    104, 116, 256 x 256 125
+//            T = 300   [260, 216, 231]
+//            T = 800   330, 287, 331
+//            T = 1800  650, 583, 595
+//            T = 2600  883, 781, 784; at 4096 256 x 256 1100, pair 1190
+// The pair with two stages of LDS took [224] at T = 300, the short tile with four waves
+// 102 at T = 30; 128 x 128 in 4 waves without a neighbour 158 at T = 16, [284] at 300.
 using GradLarge = GradShape<4, 2, 2, 4, 2, 64, 1>;   // 256 x 256, 8 waves
-using GradPair = GradShape<2, 2, 2, 4, 2, 32, 2>;    // 128 x 256, 4 waves, two blocks on a CU
+using GradPair = GradShape<2, 2, 2, 4, 3, 32, 2>;    // 128 x 256, 4 waves, two blocks on a CU
+using GradShort = GradShape<4, 2, 1, 2, 4, 32, 2>;   // 128 x 128, 8 waves, two blocks on a CU
 using GradSmall = GradShape<2, 2, 2, 2, 4, 64, 1>;   // 128 x 128, 4 waves
 using GradTall32 = GradShape<4, 1, 1, 1, 4, 64, 1>;  // 128 x 32, 4 waves
 using GradTall64 = GradShape<4, 1, 1, 2, 4, 64, 1>;  // 128 x 64, 4 waves
@@ -54,7 +59,7 @@ using GradTall96 = GradShape<4, 1, 1, 3, 4, 64, 1>;  // 128 x 96, 4 waves
 using GradTall160 = GradShape<4, 1, 1, 5, 4, 64, 1>; // 128 x 160, 4 waves
 using GradTall192 = GradShape<4, 1, 1, 6, 3, 64, 1>; // 128 x 192, 4 waves
 using GradTall320 = GradShape<4, 2, 1, 5, 2, 64, 1>; // 128 x 320, 8 waves
-enum GradTile { GRAD_LARGE, GRAD_SMALL, GRAD_PAIR, GRAD_T32, GRAD_T64, GRAD_T96, GRAD_T160, GRAD_T192, GRAD_T320, GRAD_TILES };
+enum GradTile { GRAD_LARGE, GRAD_SMALL, GRAD_PAIR, GRAD_SHORT, GRAD_T32, GRAD_T64, GRAD_T96, GRAD_T160, GRAD_T192, GRAD_T320, GRAD_TILES };
 
 template <class S, GradTile T>
 struct GradShapeTag {
@@ -68,6 +73,7 @@ auto with_grad_tile(GradTile t, F f)
     switch (t) {
     case GRAD_LARGE: return f(GradShapeTag<GradLarge, GRAD_LARGE>{});
     case GRAD_PAIR: return f(GradShapeTag<GradPair, GRAD_PAIR>{});
+    case GRAD_SHORT: return f(GradShapeTag<GradShort, GRAD_SHORT>{});
     case GRAD_T32: return f(GradShapeTag<GradTall32, GRAD_T32>{});
     case GRAD_T64: return f(GradShapeTag<GradTall64, GRAD_T64>{});
     case GRAD_T96: return f(GradShapeTag<GradTall96, GRAD_T96>{});
@@ -101,12 +107,22 @@ double grad_tile_time()
     return S::BLOCKS * std::max((double)S::BM * S::BN * S::BK * 2 / 5.4e6, (double)S::STAGE_BYTES / (S::BLOCKS > 1 ? 55e3 : 50e3));
 }
 
+// Time (us) of a tile's first loads and its outputs, in a whole round of blocks.
+// Fitted to weight gradients of D = 4096, F = 14336 (outputs of 352 MB).
+template <class S>
+constexpr double grad_tile_ends(bool weight)
+{
+    if (!weight)
+        return 8.0;
+    return S::BLOCKS > 1 ? (S::BN == 256 ? 6.5 : 3.3) : (S::BN == 256 ? 11.0 : 2.5);
+}
+
 // `problems` matmuls of M x N outputs (or N x M), `segments` contractions of K
 // each, on one tile, and the estimated time: whole rounds of tiles, the rest split
 // over k where that is faster, an exchange as in split_time, and at least the time
 // that the weights take from memory.
 template <class S>
-double grad_candidate(GradStep &s, GradTile tile, int problems, int64_t M, int64_t N, int64_t K, int segments)
+double grad_candidate(GradStep &s, GradTile tile, int problems, int64_t M, int64_t N, int64_t K, int segments, bool weight)
 {
     s.tile = tile;
     s.kt_seg = (int)std::max<int64_t>(1, cdiv(K, S::BK));
@@ -120,10 +136,11 @@ double grad_candidate(GradStep &s, GradTile tile, int problems, int64_t M, int64
     s.rest = (int)(s.tiles - s.whole);
     s.splits = 1;
     s.kt_split = s.nk;
-    // A tile's first loads and its outputs, where no other block works beside it.
-    const double per = grad_tile_time<S>(), whole = s.nk * per + (S::BLOCKS > 1 ? 4.0 : 8.0);
-    double time = (double)(s.whole / round) * whole + 2.0;
+    const double per = grad_tile_time<S>();
+    double time = (double)(s.whole / round) * (s.nk * per + grad_tile_ends<S>(weight)) + 2.0;
     if (s.rest) {
+        // No other round's blocks hide a block's own latencies.
+        const double whole = s.nk * per + (S::BLOCKS > 1 ? grad_tile_ends<S>(weight) : std::max(8.0, grad_tile_ends<S>(weight)));
         double best = whole;
         const int64_t most = std::min<int64_t>(round / s.rest, std::max(1, s.nk / 2));
         const double bytes = (double)S::BM * S::BN * sizeof(float);
@@ -145,12 +162,18 @@ double grad_candidate(GradStep &s, GradTile tile, int problems, int64_t M, int64
     return std::max(time, (double)M * (double)K * segments * 2 / 5.0e6);
 }
 
-// Whether a launch may take a tile: weight gradients the pair, products with a
-// weight the tall ones.
+// Whether a launch may take a tile: weight gradients the short one and the pair,
+// products with a weight the tall ones.
 constexpr bool grad_tile_fits(GradTile t, bool weight)
 {
-    return t == GRAD_LARGE || t == GRAD_SMALL || (t == GRAD_PAIR) == weight;
+    return t == GRAD_LARGE || t == GRAD_SMALL || (t == GRAD_PAIR || t == GRAD_SHORT) == weight;
 }
+
+// Weight gradients of up to so many tokens take the short tile: a block loads one to
+// three k-tiles and stores, and what counts is how many blocks do so at once.  Those
+// of more than the second number do not: with the tokens split over several blocks
+// its k-tiles of 32 lose (D = 512, F = 1024, T = 4096: 29.3 us, 128 x 128 in 4 waves 26.0).
+constexpr int64_t kGradShortTokens = 96, kGradShortMost = 1536;
 
 // The tile with the least estimated time.  Its rows of the widest tensor are addressed
 // with 31 bits from its corner: only the tiles of up to 192 lines take every width.
@@ -161,14 +184,16 @@ inline GradStep grad_step(int problems, int64_t M, int64_t N, int64_t K, int seg
     bool found = false;
     const int64_t widest = weight ? std::max(M, N) : std::max(M, K);
     for (int t = 0; t < GRAD_TILES; ++t) {
-        if (!grad_tile_fits((GradTile)t, weight))
+        if (!grad_tile_fits((GradTile)t, weight) ||
+            (weight && K <= kGradShortTokens && t != GRAD_SHORT) ||
+            (t == GRAD_SHORT && K > kGradShortMost))
             continue;
         GradStep s;
         const double time = with_grad_tile((GradTile)t, [&](auto tag) {
             using S = typename decltype(tag)::type;
             return std::max(S::BM, S::BN) * widest * 2 >= (int64_t(1) << 31)
                        ? HUGE_VAL
-                       : grad_candidate<S>(s, (GradTile)t, problems, M, N, K, segments);
+                       : grad_candidate<S>(s, (GradTile)t, problems, M, N, K, segments, weight);
         });
         if (time < HUGE_VAL && (!found || time < best_time)) {
             found = true;

@@ -111,11 +111,13 @@ def test_activations(T, D, F, activation, beta):
 
 # (T, D, F, tile of dH, of dX, of dW): every tile of the plan, most of them with
 # whole tiles, ragged ones and split sums.
-LARGE, PAIR, SMALL, T32, T64, T96, T160, T192, T320 = (
-    "4, 2, 2, 4, 2, 64, 1", "2, 2, 2, 4, 2, 32, 2", "2, 2, 2, 2, 4, 64, 1", "4, 1, 1, 1, 4, 64, 1", "4, 1, 1, 2, 4, 64, 1",
-    "4, 1, 1, 3, 4, 64, 1", "4, 1, 1, 5, 4, 64, 1", "4, 1, 1, 6, 3, 64, 1", "4, 2, 1, 5, 2, 64, 1")
-TILES = [(3, 264, 520, T32, T32, PAIR), (260, 264, 520, None, None, SMALL), (1030, 520, 1032, T64, None, None),
-         (1030, 1032, 2056, T96, SMALL, None), (600, 520, 1032, None, T64, None), (330, 1288, 2312, None, T96, None),
+LARGE, PAIR, SMALL, SHORT, T32, T64, T96, T160, T192, T320 = (
+    "4, 2, 2, 4, 2, 64, 1", "2, 2, 2, 4, 3, 32, 2", "2, 2, 2, 2, 4, 64, 1", "4, 2, 1, 2, 4, 32, 2", "4, 1, 1, 1, 4, 64, 1",
+    "4, 1, 1, 2, 4, 64, 1", "4, 1, 1, 3, 4, 64, 1", "4, 1, 1, 5, 4, 64, 1", "4, 1, 1, 6, 3, 64, 1", "4, 2, 1, 5, 2, 64, 1")
+TILES = [(3, 264, 520, T32, T32, SHORT), (260, 264, 520, None, None, SHORT), (80, 1032, 4104, None, None, SHORT),
+         (600, 264, 520, None, None, SMALL), (3000, 264, 520, None, None, SMALL), (5000, 1032, 2056, None, None, PAIR),
+         (1030, 520, 1032, T64, None, None),
+         (1030, 1032, 2056, T96, SMALL, None), (600, 520, 1032, None, T64, None), (330, 1288, 2312, None, T96, PAIR),
          (400, 2056, 4104, None, T160, None), (520, 2056, 4104, None, T192, None), (40, 2056, 8200, T64, None, None),
          (130, 4104, 8200, T160, T160, None), (180, 4104, 8200, T192, T192, None), (300, 4104, 8200, T320, T320, None),
          (100, 4104, 8200, SMALL, None, None), (600, 4104, 8200, LARGE, None, None), (400, 4104, 8200, None, LARGE, None),
