@@ -208,15 +208,12 @@ __device__ __forceinline__ void gate_gradients(const float (&dh)[8], const u32x4
 
 // One block: one output tile, or one split of its k-tiles.  KC: both operands
 // k-contiguous; SEGS = 2: dX's two pairs; otherwise a problem per range of
-// problem_tiles tiles.
-template <class S, bool KC, int EPI, int SEGS>
+// problem_tiles tiles.  STREAM_OUT: outputs past the L2.
+template <class S, bool KC, int EPI, int SEGS, bool STREAM_OUT>
 __global__ __launch_bounds__(S::NTHREADS, S::BLOCKS) void gemm_grad_kernel(GradParams p)
 {
     constexpr int TM = S::TM, TN = S::TN, STAGES = S::STAGES, BK = S::BK;
-    // Blocks that store beside others' loads leave the L2 to the operands: with ordinary
-    // stores the weight gradients of T = 100 took 138 us, 111 so, of 300 up to 3% more.
-    // The large tile's, after all its loads, take 3% longer so (T = 4096).
-    constexpr int OUT_POLICY = S::BLOCKS > 1 ? kNonTemporal : 0;
+    constexpr int OUT_POLICY = STREAM_OUT ? kNonTemporal : 0;
     __shared__ __attribute__((aligned(1024))) uint8_t lds0[S::STAGE_BYTES];
     __shared__ __attribute__((aligned(1024))) uint8_t lds1[S::STAGE_BYTES];
     __shared__ __attribute__((aligned(1024))) uint8_t lds2[STAGES > 2 ? S::STAGE_BYTES : 16];

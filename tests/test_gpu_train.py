@@ -185,6 +185,22 @@ def test_widest_tensors(T):
     check("dx", dx, total[0], total[1])
 
 
+@pytest.mark.parametrize("T,D,F", [(20, 256, 512), (200, 1024, 4096), (130, 4096, 8192)])
+def test_outputs_off_their_lines(T, D, F):
+    """Weight gradients that start inside a 128-byte line, and those that start on one."""
+    assert train.describe(T, D, F)[2][0].endswith("true>")
+    t = {k: v.cuda() for k, v in inputs(T, D, F, 4).items()}
+    _, g, u = train.forward(t["x"], t["wg"], t["wu"], t["wd"])
+    args = (t["dy"], t["x"], t["wg"], t["wu"], t["wd"], g, u)
+    want = run(T, D, F, seed=4)[3]
+    for off in (8, 40):
+        room = [torch.full((D * F + 128,), 7.0, dtype=torch.bfloat16, device="cuda") for _ in range(3)]
+        outs = [b[off:off + D * F].view(shape) for b, shape in zip(room, ((D, F), (D, F), (F, D)))]
+        got = train.backward(*args, dwg=outs[0], dwu=outs[1], dwd=outs[2])
+        assert all(torch.equal(a, b) for a, b in zip(got, want))
+        assert all((b[:off] == 7).all() and (b[off + D * F:] == 7).all() for b in room)
+
+
 @pytest.mark.parametrize("want", [("dx",), ("dwd",), ("dwg", "dwu"), ("dx", "dwu"), ()])
 def test_wanted_gradients_only(want):
     run(70, 264, 520, want=want, seed=9)
