@@ -206,6 +206,22 @@ __device__ __forceinline__ void gate_gradients(const float (&dh)[8], const u32x4
     }
 }
 
+// Two neighbouring runs of 32 columns of 16 rows, 16 bytes per lane each, lane l row
+// l % 16, become the first and the last eight rows with all 64 columns: 128-byte lines
+// are written whole by one store.  Rows r < 8 give their second run for the first run
+// of rows r + 8.
+__device__ __forceinline__ void store_lines(u32x4 &first, u32x4 &second, int lane)
+{
+    const bool high = lane & 8;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const uint32_t a = first[i], b = second[i];
+        const uint32_t got = __builtin_amdgcn_update_dpp(0, high ? a : b, 0x128, 0xf, 0xf, false); // row_ror:8
+        first[i] = high ? got : a;
+        second[i] = high ? b : got;
+    }
+}
+
 // One block: one output tile, or one split of its k-tiles.  KC: both operands
 // k-contiguous; SEGS = 2: dX's two pairs; otherwise a problem per range of
 // problem_tiles tiles.  STREAM_OUT: outputs past the L2.
@@ -370,6 +386,13 @@ __global__ __launch_bounds__(S::NTHREADS, S::BLOCKS) void gemm_grad_kernel(GradP
         const int in = (int)(n0 + nl < N) & (int)(m0 + ml < M); // without a branch
         return in ? ((uint32_t)nl * (uint32_t)M + (uint32_t)ml) * 2u : kOutOfRange;
     };
+    // Of a pair of runs: store `half` takes eight rows of 128 bytes (store_lines).
+    auto line_offset = [&](int b, int mi, int half) __attribute__((always_inline)) {
+        const int ml = wm * TM * 32 + mi * 32 + wide_column(lane) + 4 * (lane & 8);
+        const int nl = wn * TN * 32 + b * 16 + 8 * half + (lane & 7);
+        const int in = (int)(n0 + nl < N) & (int)(m0 + ml < M);
+        return in ? ((uint32_t)nl * (uint32_t)M + (uint32_t)ml) * 2u : kOutOfRange;
+    };
     struct Gates {
         u32x4 g[TM], u[TM];
     };
@@ -385,12 +408,13 @@ __global__ __launch_bounds__(S::NTHREADS, S::BLOCKS) void gemm_grad_kernel(GradP
     };
     // lo, hi: the two MFMA results of each run.
     auto emit = [&](int b, const f32x4 (&lo)[TM], const f32x4 (&hi)[TM]) __attribute__((always_inline)) {
+        u32x4 c[TM];
 #pragma unroll
         for (int mi = 0; mi < TM; ++mi) {
             float v[8];
             wide_columns(lo[mi], hi[mi], v);
-            const uint32_t off = offset(b, mi);
             if constexpr (EPI == GRAD_GATE) {
+                const uint32_t off = offset(b, mi);
                 const Gates &gu = gates[b % AHEAD];
                 u32x4 dg, du, h;
                 gate_gradients(v, gu.g[mi], gu.u[mi], p.activation, p.beta, dg, du, h);
@@ -398,10 +422,21 @@ __global__ __launch_bounds__(S::NTHREADS, S::BLOCKS) void gemm_grad_kernel(GradP
                 __builtin_amdgcn_raw_buffer_store_b128(du, rdu, off, 0, 0);
                 __builtin_amdgcn_raw_buffer_store_b128(h, rh, off, 0, 0);
             } else {
-                __builtin_amdgcn_raw_buffer_store_b128(u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]),
-                                                             pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])},
-                                                       ro, off, 0, OUT_POLICY);
+                c[mi] = u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
             }
+        }
+        if constexpr (EPI == GRAD_STORE && TM % 2 == 0) {
+#pragma unroll
+            for (int mi = 0; mi < TM; mi += 2) {
+                store_lines(c[mi], c[mi + 1], lane);
+#pragma unroll
+                for (int half = 0; half < 2; ++half)
+                    __builtin_amdgcn_raw_buffer_store_b128(c[mi + half], ro, line_offset(b, mi, half), 0, OUT_POLICY);
+            }
+        } else if constexpr (EPI == GRAD_STORE) {
+#pragma unroll
+            for (int mi = 0; mi < TM; ++mi)
+                __builtin_amdgcn_raw_buffer_store_b128(c[mi], ro, offset(b, mi), 0, OUT_POLICY);
         }
         if constexpr (EPI == GRAD_GATE)
             if (b + AHEAD < BATCHES)

@@ -51,7 +51,7 @@ namespace {
 // 102 at T = 30; 128 x 128 in 4 waves without a neighbour 158 at T = 16, [284] at 300.
 using GradLarge = GradShape<4, 2, 2, 4, 2, 64, 1>;   // 256 x 256, 8 waves
 using GradPair = GradShape<2, 2, 2, 4, 3, 32, 2>;    // 128 x 256, 4 waves, two blocks on a CU
-using GradShort = GradShape<4, 2, 1, 2, 4, 32, 2>;   // 128 x 128, 8 waves, two blocks on a CU
+using GradShort = GradShape<2, 4, 2, 1, 4, 32, 2>;   // 128 x 128, 8 waves, two blocks on a CU
 using GradSmall = GradShape<2, 2, 2, 2, 4, 64, 1>;   // 128 x 128, 4 waves
 using GradTall32 = GradShape<4, 1, 1, 1, 4, 64, 1>;  // 128 x 32, 4 waves
 using GradTall64 = GradShape<4, 1, 1, 2, 4, 64, 1>;  // 128 x 64, 4 waves
