@@ -26,8 +26,8 @@
 // Where there are many tokens the kernels are bound by the rate at which operand
 // tiles reach LDS and leave it again, 128 FLOP per staged byte for the 256 x 256
 // tiles; where there are few, by the weights read (dH, dX) and the gradients written.
-// Measured (us): T = 4096, D = 4096, F = 14336 dH 541, dX 671 (1.43 PFLOP/s), dW
-// 1100 (1.31 PFLOP/s).  Tried without gain for the large tiles: k-tiles of 32 in four
+// Measured (us): T = 4096, D = 4096, F = 14336 dH 512, dX 690 (1.39 PFLOP/s), dW
+// 1190 (1.21 PFLOP/s); T = 30 dW 74 (outputs of 352 MB: 4.8 TB/s).  Tried without gain for the large tiles: k-tiles of 32 in four
 // stages (dX +11%); a persistent grid that loads the next tile's operands during the
 // outputs (its control flow cost 0.2 us a k-tile, more than the loads it hid).
 #pragma once

@@ -35,20 +35,21 @@ namespace {
 // Tiles of the gradient matmuls.  The tall ones are for the products with a
 // weight (dH, dX) of few tokens: 128 rows of the weight against all the tokens, so
 // that each weight element is staged once.  The pair and the short tile are for weight
-// gradients of few tokens: the stores and first loads of one block go on beside the
-// MFMAs of the other.  Measured, us, dH and dX for each tile and dW (D = 4096, F = 14336;
+// gradients of few tokens and of small weights: the stores and first loads of one block
+// go on beside the MFMAs of the other.  Measured, us, dH and dX for each tile and dW (D = 4096, F = 14336;
 // in brackets D = 5120, F = 13824):
 //   dH + dX  T = 16    128 x 32 83, 64 86, 128 89, 192 96, 320 111, 256 x 256 112
 //            T = 64    128 x 64 95, 32 108 (dX), 128 100, 256 x 256 147 (dX)
 //            T = 300   [dX: 128 x 160 104, 320 107, 128 107, 256 x 256 129]
-//   dW       T = 30    short 90, pair 117
-//            T = 80    104, 116, 256 x 256 125
-//            T = 300   [260, 216, 231]
-//            T = 800   330, 287, 331
-//            T = 1800  650, 583, 595
-//            T = 2600  883, 781, 784; at 4096 256 x 256 1100, pair 1190
-// The pair with two stages of LDS took [224] at T = 300, the short tile with four waves
-// 102 at T = 30; 128 x 128 in 4 waves without a neighbour 158 at T = 16, [284] at 300.
+//   dW       T = 30    pair 74, 256 x 256 86, short 92
+//            T = 96    85, 104, 105
+//            T = 300   [183, 182]
+//            T = 1200  377, 377
+//            T = 2000  621, 609
+//            T = 4096  1195, 1192
+//            T = 100, D = 512, F = 1024  pair 7.0, short 5.1
+// The pair with two stages of LDS is 4% slower from T = 300 on; the short tile with four
+// waves 12% at T = 30.
 using GradLarge = GradShape<4, 2, 2, 4, 2, 64, 1>;   // 256 x 256, 8 waves
 using GradPair = GradShape<2, 2, 2, 4, 3, 32, 2>;    // 128 x 256, 4 waves, two blocks on a CU
 using GradShort = GradShape<2, 4, 2, 1, 4, 32, 2>;   // 128 x 128, 8 waves, two blocks on a CU
@@ -114,7 +115,7 @@ constexpr double grad_tile_ends(bool weight)
 {
     if (!weight)
         return 8.0;
-    return S::BLOCKS > 1 ? (S::BN == 256 ? 6.5 : 3.3) : (S::BN == 256 ? 11.0 : 2.5);
+    return S::BLOCKS > 1 ? (S::BN == 256 ? 4.5 : 3.7) : (S::BN == 256 ? 7.2 : 2.5);
 }
 
 // `problems` matmuls of M x N outputs (or N x M), `segments` contractions of K
@@ -169,11 +170,9 @@ constexpr bool grad_tile_fits(GradTile t, bool weight)
     return t == GRAD_LARGE || t == GRAD_SMALL || (t == GRAD_PAIR || t == GRAD_SHORT) == weight;
 }
 
-// Weight gradients of up to so many tokens take the short tile: a block loads one to
-// three k-tiles and stores, and what counts is how many blocks do so at once.  Those
-// of more than the second number do not: with the tokens split over several blocks
-// its k-tiles of 32 lose (D = 512, F = 1024, T = 4096: 29.3 us, 128 x 128 in 4 waves 26.0).
-constexpr int64_t kGradShortTokens = 96, kGradShortMost = 1536;
+// Most tokens of the short tile: with the tokens split over several blocks its k-tiles
+// of 32 lose (D = 512, F = 1024, T = 4096: 29.3 us, 128 x 128 in 4 waves 26.0).
+constexpr int64_t kGradShortMost = 1536;
 
 // The tile with the least estimated time.  Its rows of the widest tensor are addressed
 // with 31 bits from its corner: only the tiles of up to 192 lines take every width.
@@ -184,9 +183,7 @@ inline GradStep grad_step(int problems, int64_t M, int64_t N, int64_t K, int seg
     bool found = false;
     const int64_t widest = weight ? std::max(M, N) : std::max(M, K);
     for (int t = 0; t < GRAD_TILES; ++t) {
-        if (!grad_tile_fits((GradTile)t, weight) ||
-            (weight && K <= kGradShortTokens && t != GRAD_SHORT) ||
-            (t == GRAD_SHORT && K > kGradShortMost))
+        if (!grad_tile_fits((GradTile)t, weight) || (t == GRAD_SHORT && K > kGradShortMost))
             continue;
         GradStep s;
         const double time = with_grad_tile((GradTile)t, [&](auto tag) {

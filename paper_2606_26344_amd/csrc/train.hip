@@ -110,12 +110,10 @@ int run_save(const Step &s, const void *X, const void *Wg, const void *Wu, void 
     }
 }
 
-// Whether a launch's outputs go past the L2: where blocks store beside others' loads,
-// this leaves it to the operands.  Only outputs in whole 128-byte lines: lines that two
-// tiles share must meet in the L2.  Weight gradients, us, past it against through it:
-// D = 4096, F = 14336, T = 100 111 against 138, F = 11136, T = 2 69 against 100; D = 4040,
-// F = 11120, T = 2 142 against 94.  The large tile, whose stores come after all its
-// loads, gains nothing (T = 4096 1218 against 1180).
+// Whether the weight gradients go past the L2, which leaves it to the operands: where
+// they are in whole 128-byte lines (lines that two tiles share must meet in the L2).
+// us, past it against through it: D = 4096, F = 14336, T = 100 88 against 132, 700 242
+// against 264, 4096 1186 against 1206; D = 4040, F = 11120, T = 2 142 against 94.
 inline bool stream_outputs(const GradParams &p)
 {
     for (int i = 0; i < 3; ++i)
@@ -140,7 +138,7 @@ int launch_grad(const GradStep &s, GradParams p, const char *what, hipStream_t s
             return fail(GMLP_ERR_INVALID_ARG, "internal: no kernel for this tile");
         else {
             auto *kernel = gemm_grad_kernel<S, KC, EPI, SEGS, false>;
-            if constexpr (S::BLOCKS > 1)
+            if constexpr (!KC)
                 if (stream_outputs(p))
                     kernel = gemm_grad_kernel<S, KC, EPI, SEGS, true>;
             hipLaunchKernelGGL(kernel, dim3((unsigned)s.blocks), dim3(S::NTHREADS), 0, st, p);
@@ -188,9 +186,8 @@ int gmlp_train_describe(int64_t T, int64_t D, int64_t F, int backward, char *buf
         if (T > 0)
             text = grad_line(g.dh, "true, 1, 1, false") + grad_line(g.dx, "true, 0, 2, false");
         // The outputs taken as starting on 128-byte lines.
-        const GradStep dw = grad_weight_step(3, T, D, F);
-        const bool beside = with_grad_tile(dw.tile, [](auto tag) { return decltype(tag)::type::BLOCKS > 1; });
-        text += grad_line(dw, beside && D % 64 == 0 && F % 64 == 0 ? "false, 0, 1, true" : "false, 0, 1, false");
+        text += grad_line(grad_weight_step(3, T, D, F),
+                          D % 64 == 0 && F % 64 == 0 ? "false, 0, 1, true" : "false, 0, 1, false");
     } else if (T > 0) {
         const Step s = train_gate_up_step(T, D, F);
         text = describe_step(s, true);

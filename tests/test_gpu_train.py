@@ -114,7 +114,7 @@ def test_activations(T, D, F, activation, beta):
 LARGE, PAIR, SMALL, SHORT, T32, T64, T96, T160, T192, T320 = (
     "4, 2, 2, 4, 2, 64, 1", "2, 2, 2, 4, 3, 32, 2", "2, 2, 2, 2, 4, 64, 1", "2, 4, 2, 1, 4, 32, 2", "4, 1, 1, 1, 4, 64, 1",
     "4, 1, 1, 2, 4, 64, 1", "4, 1, 1, 3, 4, 64, 1", "4, 1, 1, 5, 4, 64, 1", "4, 1, 1, 6, 3, 64, 1", "4, 2, 1, 5, 2, 64, 1")
-TILES = [(3, 264, 520, T32, T32, SHORT), (260, 264, 520, None, None, SHORT), (80, 1032, 4104, None, None, SHORT),
+TILES = [(3, 264, 520, T32, T32, SHORT), (260, 264, 520, None, None, SHORT), (80, 1032, 4104, None, None, PAIR),
          (600, 264, 520, None, None, SMALL), (3000, 264, 520, None, None, SMALL), (5000, 1032, 2056, None, None, PAIR),
          (1030, 520, 1032, T64, None, None),
          (1030, 1032, 2056, T96, SMALL, None), (600, 520, 1032, None, T64, None), (330, 1288, 2312, None, T96, PAIR),
