@@ -53,7 +53,8 @@ size_t gmlp_w4_packed_size(int64_t K, int64_t N, int group, int zeros);
  * Without zero points s = bf16(max |w| / 7), q = min(rint(w / s) + 8, 15); with
  * them, lo = min(0, min w), hi = max(0, max w), s = bf16((hi - lo) / 15),
  * z = rint(-lo / s), q = rint(w / s) + z, z and q clamped to 0..15.  A group of
- * zeros has s = 0 and q = z.  W must be finite.
+ * zeros has s = 0 and q = z; one with a value that is not finite has s = NaN, which
+ * makes the products of its column NaN.
  */
 int gmlp_w4_quantize(const void *W, void *Q, void *S, void *Z, int64_t K, int64_t N, int group,
                      void *stream);

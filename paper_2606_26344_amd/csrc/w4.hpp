@@ -590,13 +590,17 @@ __global__ __launch_bounds__(256) void w4_quantize_kernel(W4LayoutParams p)
         return;
     const int first = g * p.group, last = min(p.K, first + p.group);
     float lo = 0.0f, hi = 0.0f;
+    bool finite = true;
     for (int k = first; k < last; ++k) {
         const float w = __builtin_bit_cast(float, (uint32_t)p.w[(size_t)k * p.N + n] << 16);
+        finite &= __builtin_isfinite(w);
         lo = fminf(lo, w);
         hi = fmaxf(hi, w);
     }
-    const float range = p.z ? (hi - lo) / 15.0f : fmaxf(-lo, hi) / 7.0f;
-    const uint16_t bits = __builtin_bit_cast(uint16_t, (__bf16)range);
+    float range = p.z ? (hi - lo) / 15.0f : fmaxf(-lo, hi) / 7.0f;
+    if (p.z && !__builtin_isfinite(range)) // hi - lo passed the range of fp32
+        range = hi / 15.0f - lo / 15.0f;
+    const uint16_t bits = finite ? __builtin_bit_cast(uint16_t, (__bf16)range) : 0x7fc0; // NaN
     const float s = __builtin_bit_cast(float, (uint32_t)bits << 16);
     const float z = !p.z ? 8.0f : s > 0.0f ? fminf(rintf(-lo / s), 15.0f) : 0.0f;
     for (int k = first; k < last; ++k) {

@@ -141,6 +141,27 @@ def test_quantize_pack_dequantize():
         assert ((ref.float() - w.float()).abs() <= (0.5 if zeros else 1.01) * s.float()[rows] * 1.02 + 2.0 ** -8 * w.float().abs() + (s.float()[rows] if zeros else 0)).all()
 
 
+@pytest.mark.parametrize("zeros", [False, True])
+def test_quantize_weights_that_are_not_finite_or_very_large(zeros):
+    K, N, group = 200, 40, 64
+    gen = torch.Generator().manual_seed(8)
+    w = torch.randn((K, N), generator=gen).to(torch.bfloat16)
+    w[70, 3], w[0, 5], w[199, 7] = float("nan"), float("inf"), float("-inf")
+    large = torch.finfo(torch.bfloat16).max
+    w[:64, 9], w[1, 9] = large, -large  # hi - lo is beyond fp32
+    q, s, z = w4.quantize(w.cuda(), group, zeros)
+    assert torch.equal(s.cpu().isnan().nonzero(), torch.tensor([[0, 5], [1, 3], [3, 7]]))
+    assert s[0, 9].isfinite() and s[0, 9] > large / 16
+    assert int(q.max()) <= 15 and (z is None or int(z.max()) <= 15)
+    p = w4.pack(q, s, z, group=group)
+    y = w4.matmul(torch.ones((3, K), dtype=torch.bfloat16, device="cuda") * 2.0 ** -10, p).cpu()
+    bad = torch.zeros(N, dtype=torch.bool)
+    bad[[3, 5, 7]] = True
+    assert torch.equal(y.isnan(), bad.expand(3, N)) and y[:, ~bad].isfinite().all()
+    d = w4.dequantize(p).cpu().float()
+    assert d[1, 9] < -0.8 * large and d[0, 9] > 0.8 * large
+
+
 def test_tokens_do_not_mix():
     # A token with a NaN or infinity gives NaN, the others the same bits; tokens
     # are the same alone and in a batch of the same size class.
