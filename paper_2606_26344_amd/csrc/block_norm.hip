@@ -184,8 +184,8 @@ int gmlp_block_norm_backward(const void *dXn, const void *dR, const void *Y, con
     const bool rows = T > 0, gate_rows = flags & GMLP_NORM_GATE_ROWS;
     if ((rc = check_norm_shape(T, D)) ||
         (rows && (rc = check_norm_args(flags, res_scale, eps, Y, w_post, gate))) || (rc = check_ptr(dXn, "dXn", rows)) ||
-        (rc = check_ptr(dR, "dR", false)) || (rc = check_ptr(Y, "Y", false)) || (rc = check_ptr(R, "R", rows)) || (rc = check_ptr(w_pre, "w_pre", false)) ||
-        (rc = check_ptr(w_post, "w_post", false)) || (rc = check_ptr(gate, "gate", false)) ||
+        (rc = check_ptr(dR, "dR", false)) || (rc = check_ptr(Y, "Y", false)) || (rc = check_ptr(R, "R", rows)) ||
+        (rc = check_ptr(w_pre, "w_pre", false)) || (rc = check_ptr(w_post, "w_post", false)) || (rc = check_ptr(gate, "gate", false)) ||
         (rc = check_ptr(dY, "dY", false)) || (rc = check_ptr(dres, "dres", false)) ||
         (rc = check_ptr(dw_pre, "dw_pre", false)) || (rc = check_ptr(dw_post, "dw_post", false)) ||
         (rc = check_ptr(dgate, "dgate", false)))

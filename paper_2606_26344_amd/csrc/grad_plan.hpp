@@ -36,8 +36,8 @@ namespace {
 // weight (dH, dX) of few tokens: 128 rows of the weight against all the tokens, so
 // that each weight element is staged once.  The pair and the short tile are for weight
 // gradients of few tokens and of small weights: the stores and first loads of one block
-// go on beside the MFMAs of the other.  Measured, us, dH and dX for each tile and dW (D = 4096, F = 14336;
-// in brackets D = 5120, F = 13824):
+// go on beside the MFMAs of the other.  Measured, us, dH and dX for each tile and dW
+// (D = 4096, F = 14336; in brackets D = 5120, F = 13824):
 //   dH + dX  T = 16    128 x 32 83, 64 86, 128 89, 192 96, 320 111, 256 x 256 112
 //            T = 64    128 x 64 95, 32 108 (dX), 128 100, 256 x 256 147 (dX)
 //            T = 300   [dX: 128 x 160 104, 320 107, 128 107, 256 x 256 129]
@@ -60,7 +60,11 @@ using GradTall96 = GradShape<4, 1, 1, 3, 4, 64, 1>;  // 128 x 96, 4 waves
 using GradTall160 = GradShape<4, 1, 1, 5, 4, 64, 1>; // 128 x 160, 4 waves
 using GradTall192 = GradShape<4, 1, 1, 6, 3, 64, 1>; // 128 x 192, 4 waves
 using GradTall320 = GradShape<4, 2, 1, 5, 2, 64, 1>; // 128 x 320, 8 waves
-enum GradTile { GRAD_LARGE, GRAD_SMALL, GRAD_PAIR, GRAD_SHORT, GRAD_T32, GRAD_T64, GRAD_T96, GRAD_T160, GRAD_T192, GRAD_T320, GRAD_TILES };
+enum GradTile {
+    GRAD_LARGE, GRAD_SMALL, GRAD_PAIR, GRAD_SHORT,
+    GRAD_T32, GRAD_T64, GRAD_T96, GRAD_T160, GRAD_T192, GRAD_T320,
+    GRAD_TILES
+};
 
 template <class S, GradTile T>
 struct GradShapeTag {
@@ -105,7 +109,8 @@ struct GradStep {
 template <class S>
 double grad_tile_time()
 {
-    return S::BLOCKS * std::max((double)S::BM * S::BN * S::BK * 2 / 5.4e6, (double)S::STAGE_BYTES / (S::BLOCKS > 1 ? 55e3 : 50e3));
+    return S::BLOCKS * std::max((double)S::BM * S::BN * S::BK * 2 / 5.4e6,
+                                (double)S::STAGE_BYTES / (S::BLOCKS > 1 ? 55e3 : 50e3));
 }
 
 // Time (us) of a tile's first loads and its outputs, in a whole round of blocks.
@@ -147,7 +152,8 @@ double grad_candidate(GradStep &s, GradTile tile, int problems, int64_t M, int64
         const double bytes = (double)S::BM * S::BN * sizeof(float);
         for (int64_t n = 2; n <= most; ++n) {
             const int64_t kt = cdiv(s.nk, n), splits = cdiv(s.nk, kt);
-            const double t = (double)kt * per + (whole - s.nk * per) + 4.0 + (double)splits * bytes / 54e3 + (double)(splits * s.rest) * bytes / 8e6;
+            const double t = (double)kt * per + (whole - s.nk * per) + 4.0 + (double)splits * bytes / 54e3 +
+                             (double)(splits * s.rest) * bytes / 8e6;
             if (t < best) {
                 best = t;
                 s.kt_split = (int)kt;

@@ -41,7 +41,9 @@ int check_apart(const Span *in, int n_in, const Span *out, int n_out, const void
 
 int check_train_path(int path)
 {
-    return path == GMLP_PATH_AUTO ? GMLP_OK : fail(GMLP_ERR_INVALID_ARG, "the training step has the automatic path only (got %d)", path);
+    return path == GMLP_PATH_AUTO
+               ? GMLP_OK
+               : fail(GMLP_ERR_INVALID_ARG, "the training step has the automatic path only (got %d)", path);
 }
 
 // One launch of a GEMM kernel takes fewer than 2^32 threads.
