@@ -483,8 +483,14 @@ __global__ __launch_bounds__(S::NTHREADS, S::BLOCKS) void gemm_grad_kernel(GradP
         if (tid == 0)
             __hip_atomic_store(p.counters + piece_tile, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
         first_gates();
-        // GROUP batches' sums at once, so that more loads are in flight.
-        constexpr int GROUP = TM == 1 && BATCHES % 4 == 0 ? 4 : 2;
+        // GROUP batches' sums at once: the loads of one split, of up to 20 pieces, are in
+        // flight together, and each split costs their latency (about 2 us) for every group.
+        constexpr int GROUP = [] {
+            int g = BATCHES;
+            while (g * 2 * TM > 20 || BATCHES % g)
+                --g;
+            return g;
+        }();
 #pragma unroll
         for (int b0 = 0; b0 < BATCHES; b0 += GROUP) {
             f32x4 sum[GROUP][2][TM];
