@@ -135,7 +135,7 @@ double grad_candidate(GradStep &s, GradTile tile, int problems, int64_t M, int64
     s.nk = segments * s.kt_seg;
     s.threads = S::NTHREADS;
     s.tiles = 0;
-    for (int i = 0; i < problems; ++i) // the third weight gradient is the transposed shape
+    for (int i = 0; i < problems; ++i) // among several, dWd is the transposed shape
         s.tiles += std::max(cdiv(M, S::BM) * cdiv(N, S::BN), problems > 1 ? cdiv(N, S::BM) * cdiv(M, S::BN) : 0);
     const int64_t round = (int64_t)S::BLOCKS * kBlockTarget;
     s.whole = s.tiles / round * round;
@@ -219,8 +219,16 @@ inline GradPlan grad_plan(int64_t T, int64_t D, int64_t F)
     return p;
 }
 
-// The weight gradients, as many as are wanted.
-inline GradStep grad_weight_step(int problems, int64_t T, int64_t D, int64_t F) { return grad_step(problems, F, D, T, 1, true); }
+// The weight gradients that are wanted, as problems of one launch.  dWg and dWu have F
+// columns and D rows, dWd D columns and F rows; several problems take the tiles of the
+// orientation that has more.
+inline GradStep grad_weight_step(bool dwg, bool dwu, bool dwd, int64_t T, int64_t D, int64_t F)
+{
+    const int problems = (int)dwg + (int)dwu + (int)dwd;
+    const bool down_alone = dwd && problems == 1;
+    return grad_step(problems, down_alone ? D : F, down_alone ? F : D, T, 1, true);
+}
+inline GradStep grad_weight_step(int64_t T, int64_t D, int64_t F) { return grad_weight_step(true, true, true, T, D, F); }
 
 // The gate/up step of the training forward pass: the forward pass's tiles that hold
 // both weights, with H, G and U in the epilogue.
@@ -252,8 +260,8 @@ inline TrainLayout train_layout(int64_t T, int64_t D, int64_t F)
     const Step s = train_gate_up_step(T, D, F);
     size_t partial = std::max({s.partial_bytes, g.dh.partial_bytes, g.dx.partial_bytes});
     l.counters = std::max({l.fwd.counters, s.counters, g.dh.counters, g.dx.counters});
-    for (int problems = 1; problems <= 3; ++problems) { // calls may want one, two or three of the weight gradients
-        const GradStep dw = grad_weight_step(problems, T, D, F);
+    for (int want : {1, 3, 4, 7}) { // calls may want any of the weight gradients: dWg or dWu, two, dWd, all
+        const GradStep dw = grad_weight_step(want & 1, want & 2, want & 4, T, D, F);
         partial = std::max(partial, dw.partial_bytes);
         l.counters = std::max(l.counters, dw.counters);
     }

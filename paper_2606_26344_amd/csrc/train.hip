@@ -60,7 +60,7 @@ int check_train_shape(int64_t T, int64_t D, int64_t F)
     if ((rc = check_shape(T, D, F)))
         return rc;
     const GradPlan g = grad_plan(std::max<int64_t>(T, 1), D, F);
-    if ((rc = check_grid(g.dh)) || (rc = check_grid(g.dx)) || (rc = check_grid(grad_weight_step(3, T, D, F))))
+    if ((rc = check_grid(g.dh)) || (rc = check_grid(g.dx)) || (rc = check_grid(grad_weight_step(T, D, F))))
         return rc;
     return GMLP_OK;
 }
@@ -188,7 +188,7 @@ int gmlp_train_describe(int64_t T, int64_t D, int64_t F, int backward, char *buf
         if (T > 0)
             text = grad_line(g.dh, "true, 1, 1, false") + grad_line(g.dx, "true, 0, 2, false");
         // The outputs taken as starting on 128-byte lines.
-        text += grad_line(grad_weight_step(3, T, D, F),
+        text += grad_line(grad_weight_step(T, D, F),
                           D % 64 == 0 && F % 64 == 0 ? "false, 0, 1, true" : "false, 0, 1, false");
     } else if (T > 0) {
         const Step s = train_gate_up_step(T, D, F);
@@ -265,7 +265,7 @@ int gmlp_train_backward(const void *dY, const void *X, const void *Wg, const voi
     uint16_t *H = reinterpret_cast<uint16_t *>(ws + l.fwd.h_off);
     uint16_t *dG = reinterpret_cast<uint16_t *>(ws + l.dg_off), *dU = reinterpret_cast<uint16_t *>(ws + l.du_off);
     const GradPlan plan = grad_plan(std::max<int64_t>(T, 1), D, F);
-    const GradStep dw = problems ? grad_weight_step(problems, T, D, F) : GradStep{};
+    const GradStep dw = problems ? grad_weight_step(dWg, dWu, dWd, T, D, F) : GradStep{};
     if ((rc = clear_counters(fresh, std::max({plan.dh.counters, plan.dx.counters, dw.counters}), ws, l.fwd, st)))
         return rc;
 
