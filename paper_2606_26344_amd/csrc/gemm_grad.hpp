@@ -182,7 +182,9 @@ struct GradFragments {
     }
 };
 
-// dG, dU and H of eight neighbouring elements.
+// dG, dU and H of eight neighbouring elements.  sigmoid' = s (1 - s); above zero, where s
+// nears 1 and the difference would lose its digits (at g = 16 all of them), 1 - s is
+// e^-bg s.
 __device__ __forceinline__ void gate_gradients(const float (&dh)[8], const u32x4 &g4, const u32x4 &u4, int act, float beta,
                                                u32x4 &dg4, u32x4 &du4, u32x4 &h4)
 {
@@ -192,8 +194,8 @@ __device__ __forceinline__ void gate_gradients(const float (&dh)[8], const u32x4
 #pragma unroll
         for (int e = 0; e < 2; ++e) {
             const float g = e ? bf16_hi(g4[q]) : bf16_lo(g4[q]), u = e ? bf16_hi(u4[q]) : bf16_lo(u4[q]);
-            const float s = __builtin_amdgcn_rcpf(1.0f + __expf(-(beta * g)));
-            const float c = s * (1.0f - s); // sigmoid'
+            const float x = beta * g, t = __expf(-x), s = __builtin_amdgcn_rcpf(1.0f + t);
+            const float c = s * (x > 0.0f ? t * s : 1.0f - s); // sigmoid'
             const bool glu = act == ACT_SIGMOID;
             const float a = glu ? s : g * s;
             const float da = glu ? c : s + beta * g * c;
