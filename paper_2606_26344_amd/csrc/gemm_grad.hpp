@@ -184,7 +184,8 @@ struct GradFragments {
 
 // dG, dU and H of eight neighbouring elements.  sigmoid' = s (1 - s); above zero, where s
 // nears 1 and the difference would lose its digits (at g = 16 all of them), 1 - s is
-// e^-bg s.
+// e^-bg s.  beta g may be infinite where g is not, and s (1 - s) is 0 then: beta comes
+// after it.
 __device__ __forceinline__ void gate_gradients(const float (&dh)[8], const u32x4 &g4, const u32x4 &u4, int act, float beta,
                                                u32x4 &dg4, u32x4 &du4, u32x4 &h4)
 {
@@ -198,7 +199,7 @@ __device__ __forceinline__ void gate_gradients(const float (&dh)[8], const u32x4
             const float c = s * (x > 0.0f ? t * s : 1.0f - s); // sigmoid'
             const bool glu = act == ACT_SIGMOID;
             const float a = glu ? s : g * s;
-            const float da = glu ? c : s + beta * g * c;
+            const float da = glu ? c : s + beta * c * g;
             h[e] = a * u;
             du[e] = dh[2 * q + e] * a;
             dg[e] = dh[2 * q + e] * u * da;

@@ -68,3 +68,11 @@ def test_sigmoid_slope_is_even():
     v, got, *_ = slopes(torch.tensor([8.0, 12.0, 16.0, 20.0, -8.0, -12.0, -16.0, -20.0]), "sigmoid", 1.0)
     assert (got[0][:4] > 0).all()
     assert ((got[0][:4] - got[0][4:]).abs() <= 2.0 ** -7 * got[0][4:]).all()  # two roundings and what is before them
+
+
+@pytest.mark.parametrize("activation,beta", VARIANTS + [("swish", 4.0), ("swish", -1e3), ("swish", 3e38)])
+def test_largest_and_smallest_gates(activation, beta):
+    """Every power of two of bf16: b g may pass the range of fp32, the slope stays 0 or 1."""
+    p = 2.0 ** torch.arange(-124, 128, dtype=torch.float64)
+    large = torch.finfo(torch.bfloat16).max
+    check(torch.cat([p, -p, torch.tensor([large, -large, 0.0, -0.0, 1.0, -1.0, 3.0, -3.0], dtype=torch.float64)]), activation, beta)
