@@ -48,8 +48,8 @@ extern "C" {
 /*
  * Bytes of workspace both calls below need for this shape: H, dG and dU, the
  * fp32 split-K partial sums and the counter block that gmlp_workspace_init
- * prepares.  0 if the shape is invalid.  It also serves the entry points of
- * gmlp.h on the same shape.
+ * prepares.  0 if the shape is invalid.  Enough for fewer tokens too, and for the
+ * entry points of gmlp.h on these shapes.
  */
 size_t gmlp_train_workspace_size(int64_t T, int64_t D, int64_t F);
 

@@ -272,5 +272,28 @@ inline TrainLayout train_layout(int64_t T, int64_t D, int64_t F)
     return l;
 }
 
+// A bound of the partial sums of every step of up to T tokens.  The blocks of a split
+// launch are one round, 256 of at most 256 x 256 fp32 sums or 512 of half as many; and
+// there are at most K / 64 splits (the GEMV kernels', of 16 rows, hold 8 tokens) of the
+// outputs rounded up to tiles.  The fused paths hold both steps' sums at once.
+inline size_t most_partial(int64_t T, int64_t D, int64_t F)
+{
+    const auto sums = [](int64_t columns, int64_t rows, int64_t K) {
+        return (double)(columns + 255) * (double)(rows + 319) * (double)cdiv(K, 64) * sizeof(float);
+    };
+    const double steps = 2.0 * sums(F, T, D) + sums(D, T, F); // gate/up (and dH), down (and dX)
+    const double weights = T > 64 ? 3.0 * sums(F, D, T) : 0.0;
+    return (size_t)std::min(std::max(steps, weights), 64.0 * 1024 * 1024);
+}
+
+// The workspace of calls of up to T tokens: shorter sequences may split their sums more.
+inline size_t train_workspace_bytes(int64_t T, int64_t D, int64_t F)
+{
+    const TrainLayout l = train_layout(T, D, F);
+    T = std::max<int64_t>(T, 1);
+    return std::max(l.total, l.fwd.partial_off + align_up(most_partial(T, D, F)) + align_up((size_t)T * sizeof(float)) +
+                                 2 * align_up((size_t)T * F * 2));
+}
+
 } // namespace
 } // namespace gmlp

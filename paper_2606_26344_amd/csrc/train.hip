@@ -171,7 +171,7 @@ size_t gmlp_train_workspace_size(int64_t T, int64_t D, int64_t F)
 {
     if (check_train_shape(T, D, F))
         return 0;
-    return train_layout(T, D, F).total;
+    return train_workspace_bytes(T, D, F);
 }
 
 int gmlp_train_describe(int64_t T, int64_t D, int64_t F, int backward, char *buf, size_t bytes)

@@ -31,7 +31,7 @@ def workspace_size(T: int, D: int, F: int) -> int:
 
 
 def make_workspace(T: int, D: int, F: int, device=None, stream=None) -> Workspace:
-    """A zeroed workspace that fits forward() and backward() of this shape."""
+    """A zeroed workspace that fits forward() and backward() of up to T tokens."""
     n = workspace_size(T, D, F)
     if n == 0:
         raise ValueError("invalid shape T=%d D=%d F=%d" % (T, D, F))

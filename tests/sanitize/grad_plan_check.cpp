@@ -79,6 +79,24 @@ static void check_shape_plans(int64_t T, int64_t D, int64_t F)
            "T=%lld D=%lld F=%lld: dG and dU", (long long)T, (long long)D, (long long)F);
 }
 
+// A workspace made for T tokens holds every call of fewer.
+static void check_fewer_tokens(int64_t D, int64_t F, const std::vector<int64_t> &Ts)
+{
+    size_t most = 0, before = 0;
+    for (int64_t T : Ts) {
+        if (check_shape(T, D, F) != GMLP_OK)
+            return;
+        most = std::max(most, train_layout(T, D, F).total);
+        const size_t size = train_workspace_bytes(T, D, F);
+        EXPECT(size >= most, "T=%lld D=%lld F=%lld: %zu bytes, %zu for it or fewer tokens", (long long)T, (long long)D, (long long)F,
+               size, most);
+        EXPECT(size >= before && size >= make_layout(T, D, F).total, "T=%lld D=%lld F=%lld", (long long)T, (long long)D, (long long)F);
+        // Not more than the round of split tiles above what T itself takes.
+        EXPECT(size <= train_layout(T, D, F).total + ((size_t)64 << 20) + 512, "%zu bytes", size);
+        before = size;
+    }
+}
+
 int main()
 {
     const std::vector<int64_t> Ts = {0, 1, 16, 30, 33, 64, 100, 130, 300, 520, 700, 1536, 1537, 2000, 4096, 8192, 1 << 20};
@@ -93,6 +111,16 @@ int main()
     };
     for (int i = 0; i < 4000; ++i)
         check_shape_plans(random(1, i % 2 ? 64 : 8192), 8 * random(1, 1024), 8 * random(1, 3584));
+    std::vector<int64_t> every;
+    for (int64_t T = 0; T <= 700; ++T)
+        every.push_back(T);
+    for (int64_t T = 705; T <= 10000; T += 37)
+        every.push_back(T);
+    for (auto [D, F] : std::vector<std::pair<int64_t, int64_t>>{{8, 8}, {256, 512}, {8, 4096}, {1024, 4096}, {2048, 8192}, {4096, 11008},
+                                                                {4096, 14336}, {5120, 13824}, {8192, 28672}, {8, 1 << 22}, {1 << 22, 8}})
+        check_fewer_tokens(D, F, every);
+    for (int i = 0; i < 60; ++i)
+        check_fewer_tokens(8 * random(1, 1024), 8 * random(1, 3584), every);
     std::printf("training plans: %d steps checked, %d failures\n", steps, failures);
     return failures ? 1 : 0;
 }
