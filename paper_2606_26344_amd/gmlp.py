@@ -265,10 +265,13 @@ def workspace_size(T: int, D: int, F: int) -> int:
 
 class Workspace:
     """A caller-owned workspace for forward(), zeroed once at creation
-    (``nbytes`` overrides the size gmlp_workspace_size gives)."""
+    (``nbytes`` overrides the size gmlp_workspace_size gives).  The
+    make_workspace() of the other modules make theirs with ``size``, their
+    workspace_size()."""
 
-    def __init__(self, T: int, D: int, F: int, device=None, stream=None, nbytes: int = 0):
-        n = nbytes or workspace_size(T, D, F)
+    def __init__(self, T: int, D: int, F: int, device=None, stream=None, nbytes: int = 0, size=None):
+        self.size = size or workspace_size
+        n = nbytes or self.size(T, D, F)
         if n == 0:
             raise ValueError("invalid shape T=%d D=%d F=%d" % (T, D, F))
         # 256 bytes of slack so the buffer can be 256-byte aligned.  Allocated
@@ -280,7 +283,9 @@ class Workspace:
         _check(library().gmlp_workspace_init(_ptr(self.buffer), n, _stream(stream)))
 
     def fits(self, T: int, D: int, F: int) -> bool:
-        return workspace_size(T, D, F) <= self.nbytes
+        """Whether it is large enough for calls of this (valid) shape of the
+        module that made it, in the order of that module's workspace_size()."""
+        return 0 < self.size(T, D, F) <= self.nbytes
 
     def fused_giveups(self, stream=None) -> int:
         """gmlp_workspace_status: read and clear the count of fused-kernel

@@ -33,7 +33,7 @@ def make_workspace(M: int, K: int, N: int, device=None, stream=None) -> Workspac
     n = workspace_size(M, K, N)
     if n == 0:
         raise ValueError("invalid shape M=%d K=%d N=%d" % (M, K, N))
-    return Workspace(M, N, K, device=device, stream=stream, nbytes=n)
+    return Workspace(M, K, N, device=device, stream=stream, nbytes=n, size=workspace_size)
 
 
 def describe(M: int, K: int, N: int, path: str = "auto") -> list:

@@ -32,10 +32,7 @@ def workspace_size(T: int, D: int, F: int) -> int:
 
 def make_workspace(T: int, D: int, F: int, device=None, stream=None) -> Workspace:
     """A zeroed workspace that fits forward() and backward() of up to T tokens."""
-    n = workspace_size(T, D, F)
-    if n == 0:
-        raise ValueError("invalid shape T=%d D=%d F=%d" % (T, D, F))
-    return Workspace(T, D, F, device=device, stream=stream, nbytes=n)
+    return Workspace(T, D, F, device=device, stream=stream, size=workspace_size)
 
 
 def describe(T: int, D: int, F: int, backward: bool = True) -> list:

@@ -48,10 +48,7 @@ def workspace_size(T: int, D: int, F: int) -> int:
 def make_workspace(T: int, D: int, F: int, device=None, stream=None) -> Workspace:
     """A prepared workspace for forward() and gate_up() with weights [D, F] and
     for matmul() with weights [D, F] or [F, D]."""
-    n = workspace_size(T, D, F)
-    if n == 0:
-        raise ValueError("invalid shape T=%d D=%d F=%d" % (T, D, F))
-    return Workspace(T, D, F, device=device, stream=stream, nbytes=n)
+    return Workspace(T, D, F, device=device, stream=stream, size=workspace_size)
 
 
 def _expect_bytes(t, name, shape, device) -> None:
