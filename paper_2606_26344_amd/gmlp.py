@@ -233,13 +233,20 @@ def _on_current(device) -> None:
         raise ValueError("the tensors are on %s, the current device is cuda:%d" % (device, torch._C._cuda_getDevice()))
 
 
-def _prepared(workspace, device):
-    """(address, bytes) of a Workspace whose counters are prepared."""
+def _owned(workspace):
+    """(address, bytes) of a Workspace, whose counters are prepared.  Memory that is
+    not, such as the norms' workspace, would leave outputs unwritten."""
     if not isinstance(workspace, Workspace):
-        raise TypeError("workspace must be one of make_workspace(), got %s" % type(workspace).__name__)
+        raise TypeError("workspace must be a gmlp.Workspace (or one of make_workspace()), got %s" % type(workspace).__name__)
+    return workspace.buffer.data_ptr(), workspace.nbytes
+
+
+def _prepared(workspace, device):
+    """_owned, on the tensors' device."""
+    at = _owned(workspace)
     if workspace.buffer.device != device:
         raise ValueError("workspace must be on %s, got %s" % (device, workspace.buffer.device))
-    return workspace.buffer.data_ptr(), workspace.nbytes
+    return at
 
 
 def describe(T: int, D: int, F: int, path: str = "auto") -> list:
@@ -341,7 +348,7 @@ def forward(x: torch.Tensor, wg: torch.Tensor, wu: torch.Tensor, wd: torch.Tenso
                             "invalid shape T=%d D=%d F=%d" % (T, D, F))
         code |= FRESH_WORKSPACE
     else:
-        keep, ws, nbytes = None, workspace.buffer.data_ptr(), workspace.nbytes
+        keep, (ws, nbytes) = None, _owned(workspace)
     if variant is None:
         _check(lib.gmlp_forward_ex(x.data_ptr(), wg.data_ptr(), wu.data_ptr(), wd.data_ptr(), out.data_ptr(), T, D, F,
                                    code, ws, nbytes, st))
@@ -392,7 +399,7 @@ def gate_up(x: torch.Tensor, wg: torch.Tensor, wu: torch.Tensor,
         if code not in (PATH_FUSED, PATH_FUSED_MFMA):  # refused by the library
             code |= FRESH_WORKSPACE
     else:
-        keep, ws, nbytes = None, workspace.buffer.data_ptr(), workspace.nbytes
+        keep, (ws, nbytes) = None, _owned(workspace)
     if plain:
         _check(library().gmlp_gate_up_ws(x.data_ptr(), wg.data_ptr(), wu.data_ptr(), out.data_ptr(), T, D, F, code, ws,
                                          nbytes, st))
@@ -423,7 +430,7 @@ def down(h: torch.Tensor, wd: torch.Tensor, out: Optional[torch.Tensor] = None,
         if code not in (PATH_FUSED, PATH_FUSED_MFMA):  # refused by the library
             code |= FRESH_WORKSPACE
     else:
-        keep, ws, nbytes = None, workspace.buffer.data_ptr(), workspace.nbytes
+        keep, (ws, nbytes) = None, _owned(workspace)
     _check(library().gmlp_down_ws(h.data_ptr(), wd.data_ptr(), out.data_ptr(), T, F, D, code, ws, nbytes, st))
     return out
 

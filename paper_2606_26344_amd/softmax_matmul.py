@@ -21,7 +21,7 @@ from typing import Optional
 import torch
 
 from .gmlp import (_CALL_DEVICE, FRESH_WORKSPACE, PATH_AUTO, PATH_FUSED, PATH_FUSED_MFMA, _PATHS, Workspace, _check, _empty,
-                   _expect, _parse_plan, _ptr, _scratch, _stream, library)
+                   _expect, _owned, _parse_plan, _ptr, _scratch, _stream, library)
 
 
 def workspace_size(M: int, K: int, N: int) -> int:
@@ -67,7 +67,7 @@ def softmax_matmul(x: torch.Tensor, y: torch.Tensor, out: Optional[torch.Tensor]
         if code not in (PATH_FUSED, PATH_FUSED_MFMA):  # refused by the library
             code |= FRESH_WORKSPACE
     else:
-        keep, ws, nbytes = None, workspace.buffer.data_ptr(), workspace.nbytes
+        keep, (ws, nbytes) = None, _owned(workspace)
     _check(library().softmax_matmul_ws(x.data_ptr(), y.data_ptr(), out.data_ptr(), M, K, N, code, ws, nbytes, st))
     return out
 
@@ -106,6 +106,5 @@ def divide(p: torch.Tensor, s: torch.Tensor, y: torch.Tensor, out: Optional[torc
     if workspace is None:
         workspace = make_workspace(M, K, N, device=dev, stream=stream)
     _check(library().softmax_matmul_divide_ws(_ptr(p), _ptr(s), _ptr(y), _ptr(out), M, K, N,
-                                              _PATHS[path], _ptr(workspace.buffer),
-                                              workspace.nbytes, _stream(stream)))
+                                              _PATHS[path], *_owned(workspace), _stream(stream)))
     return out

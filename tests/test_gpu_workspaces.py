@@ -2,7 +2,7 @@
 import pytest
 import torch
 
-from paper_2606_26344_amd import gmlp, train, w4
+from paper_2606_26344_amd import block_norm, gmlp, train, w4
 from paper_2606_26344_amd import softmax_matmul as smm
 
 pytestmark = pytest.mark.gpu
@@ -31,3 +31,21 @@ def test_fits_is_the_makers():
     ws = smm.make_workspace(40, 264, 520)
     assert ws.fits(40, 264, 520) and not ws.fits(4000, 264, 520)
     assert not any(ws.fits(4, 260, 520) for ws in (plain, ws))  # no valid shape
+
+
+def test_the_norms_workspace_is_refused():
+    """It has no prepared counters, without which split sums are never finished."""
+    T, D, F = 40, 264, 520
+    gen = torch.Generator().manual_seed(1)
+    x, wg, wu, wd = (torch.randn(s, generator=gen).to(torch.bfloat16).cuda() for s in ((T, D), (D, F), (D, F), (F, D)))
+    h = gmlp.gate_up(x, wg, wu)
+    p, s = smm.exp_rows(h)
+    ws = block_norm.make_workspace(4096, 4096)
+    calls = [lambda ws: gmlp.forward(x, wg, wu, wd, workspace=ws), lambda ws: gmlp.gate_up(x, wg, wu, workspace=ws),
+             lambda ws: gmlp.forward(x, wg, wu, wd, workspace=ws, activation="sigmoid"),
+             lambda ws: gmlp.down(h, wd, workspace=ws), lambda ws: smm.softmax_matmul(h, wd, workspace=ws),
+             lambda ws: smm.divide(p, s, wd, workspace=ws)]
+    for call in calls:
+        with pytest.raises(TypeError, match="workspace"):
+            call(ws)
+        assert torch.isfinite(call(train.make_workspace(T, D, F)).float()).all()
