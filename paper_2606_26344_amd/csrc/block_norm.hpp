@@ -428,7 +428,8 @@ __global__ __launch_bounds__(kNormMaxThreads) void norm_backward_kernel(NormPara
 
 // Plane blockIdx.y of the partial sums, added over the blocks: 32 columns per
 // block, 16 groups of partial rows, each with 8 loads in flight; the groups' sums
-// in order.  Plane 1, times the channel gate (w_post), is dw_post (dgate).
+// in order.  Plane 1, times the channel gate (w_post), is dw_post (dgate); of no rows
+// (no blocks) all are zeros, whatever the gate is.
 struct NormColumns {
     const float *partial;
     const uint16_t *w_post, *gate; // nullptr: ones
@@ -464,9 +465,9 @@ __global__ __launch_bounds__(kNormColumns *kNormGroups) void norm_columns_kernel
         return;
     }
     if (p.dw_post)
-        p.dw_post[d] = bf16(p.gate ? s * bf16_lo(p.gate[d]) : s);
+        p.dw_post[d] = bf16(p.gate && p.blocks ? s * bf16_lo(p.gate[d]) : s);
     if (p.dgate)
-        p.dgate[d] = bf16(p.w_post ? s * bf16_lo(p.w_post[d]) : s);
+        p.dgate[d] = bf16(p.w_post && p.blocks ? s * bf16_lo(p.w_post[d]) : s);
 }
 
 } // namespace gmlp
