@@ -85,6 +85,15 @@ __device__ __forceinline__ void barrier_only()
     asm volatile("" ::: "memory");
 }
 
+// Orders a wave's LDS accesses before it against those after it, for LDS that the lanes of
+// one wave hand to each other: no instruction, since they run in order.
+__device__ __forceinline__ void wave_lds_fence()
+{
+    __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront", "local");
+    __builtin_amdgcn_wave_barrier();
+    __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront", "local");
+}
+
 // fp32 -> bf16 with round-to-nearest-even (v_cvt_pk_bf16_f32 on gfx950).
 __device__ __forceinline__ uint32_t pack_bf16x2(float lo, float hi)
 {

@@ -170,10 +170,13 @@ __global__ __launch_bounds__(WAVES * 64, 8 / WAVES) void w4_kernel(W4Params p)
     auto use = [&](const Batch &b) __attribute__((always_inline)) {
         bf16x8 x[NB][4];
         if constexpr (VIA_LDS) {
-            // The wave's own rows: its LDS operations run in order.
+            // The wave's own rows: its LDS operations run in order, and the fences
+            // tell the compiler that other lanes' rows are read (no instruction).
+            wave_lds_fence();
 #pragma unroll
             for (int i = 0; i < X_REGS; ++i)
                 *(u32x4 *)(rows + x_write + i * 1024) = b.x[i];
+            wave_lds_fence();
 #pragma unroll
             for (int j = 0; j < 4; ++j)
                 x[0][j] = *(const bf16x8 *)(rows + (x_read ^ j << 6));
