@@ -17,8 +17,10 @@
  * gmlp.h (G and U in fp32, H rounded once).  q - z is formed as the difference of
  * two products, with 1 + q/128 and with 1 + z/128, in the fp32 accumulators: a
  * token with a value that is not finite, or whose sum of |x| over a group exceeds
- * the range of fp32, gives NaN results.  Bitwise reproducible: sums are in an
- * order fixed by the shape.
+ * the range of fp32, gives NaN results, and the difference is off by up to 2^-10.8
+ * s sum |x| of its group (2^-14.5 measured), also where a large x meets a weight of 0:
+ * a value some thousand times the others of its group costs about as much as the
+ * rounding of the result.  Bitwise reproducible: sums are in an order fixed by the shape.
  *
  * Layout: X [T, K], Y [T, N], H [T, F], Q [K, N] and W [K, N] dense and row-major,
  * S and Z [ceil(K / group), N], all on the current HIP device and 16-byte aligned
