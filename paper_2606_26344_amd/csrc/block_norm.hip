@@ -39,7 +39,8 @@ NormShape norm_shape(int64_t T, int64_t D, int threads, int most_blocks)
 // Forward: blocks of up to 512 threads, as many as the CUs hold at once (3 each;
 // 4096 x 4096 26.4 us, with 2 27.7, 4 29.7, one block for every row 30.4).
 // Backward: one block of up to 1024 threads for each CU, since every block adds a row
-// of partial sums (4096 x 4096 47.3 us; two of 512 threads 49.1, three 56.4).
+// of partial sums (4096 x 4096 47.3 us; two of 512 threads 49.1, three 56.4; not measured
+// where two would save a round of rows, as at 1000).
 NormShape norm_forward_shape(int64_t T, int64_t D) { return norm_shape(T, D, 512, 3 * kBlockTarget); }
 NormShape norm_backward_shape(int64_t T, int64_t D) { return norm_shape(T, D, kNormMaxThreads, kBlockTarget); }
 

@@ -26,11 +26,12 @@
 // Where there are many tokens the kernels are bound by the rate at which operand
 // tiles reach LDS and leave it again, 128 FLOP per staged byte for the 256 x 256
 // tiles; where there are few, by the weights read (dH, dX) and the gradients written.
-// Measured (us): T = 4096, D = 4096, F = 14336 dH 512, dX 690 (1.39 PFLOP/s), dW
-// 1190 (1.21 PFLOP/s); T = 30 dW 74 (outputs of 352 MB: 4.8 TB/s).  Tried without gain
-// for the large tiles: k-tiles of 32 in four stages (dX +11%); a persistent grid that
-// loads the next tile's operands during the outputs (its control flow cost 0.2 us a
-// k-tile, more than the loads it hid).
+// Measured (us): T = 4096, D = 4096, F = 14336 dH 500 to 510 (0.96 PFLOP/s: its outputs have
+// no MFMAs beside them), dX 675 to 690 (1.41), dW 1110 to 1160 (1.27); the vendor library's
+// 8192^3 products of these operand orders reach 1.61 and 1.19.  T = 30 dW 74 (outputs of
+// 352 MB: 4.8 TB/s).  Tried without gain for the large tiles: k-tiles of 32 in four stages
+// (dX +11%); a persistent grid that loads the next tile's operands during the outputs (its
+// control flow cost 0.2 us a k-tile, more than the loads it hid).
 #pragma once
 
 #include <utility>

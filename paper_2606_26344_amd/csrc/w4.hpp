@@ -517,6 +517,8 @@ __global__ __launch_bounds__(kW4SharedWaves * 64, 1) void w4_shared_kernel(W4Par
 }
 
 // ---- laying out, rounding and restoring weights -----------------------------------
+// Once per weight; [4096, 14336], groups of 128: rounding 98 us, layout 46, restoring 26
+// ([14336, 4096] 51: a wave writes 16 columns of a row, 32 bytes).
 
 struct W4LayoutParams {
     uint8_t *tiles, *scales, *zeros; // packed
