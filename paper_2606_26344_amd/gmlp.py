@@ -34,7 +34,8 @@ HERE = os.path.dirname(os.path.abspath(__file__))
 LIBRARY = os.path.join(HERE, "libgmlp.so")
 HEADER = os.path.join(os.path.dirname(HERE), "include", "gmlp.h")
 HEADERS = [os.path.join(os.path.dirname(HERE), "include", h)
-           for h in ("gmlp.h", "softmax_matmul.h", "gmlp_train.h", "gmlp_block_norm.h", "gmlp_w4.h")]
+           for h in ("gmlp.h", "softmax_matmul.h", "gmlp_train.h", "gmlp_block_norm.h", "gmlp_w4.h",
+                     "gmlp_route.h", "gmlp_dropout.h")]
 
 PATH_AUTO, PATH_GEMV, PATH_MFMA, PATH_FUSED, PATH_FUSED_MFMA = 0, 1, 2, 3, 4
 _PATHS = {"auto": PATH_AUTO, "gemv": PATH_GEMV, "mfma": PATH_MFMA, "fused": PATH_FUSED,
@@ -49,6 +50,8 @@ _I64 = ctypes.c_int64
 _SZ = ctypes.c_size_t
 _F = ctypes.c_float
 _INT = ctypes.c_int
+_U64 = ctypes.c_uint64
+_D = ctypes.c_double
 
 _SIGNATURES = {
     "gmlp_version": ([], ctypes.c_int),
@@ -95,6 +98,12 @@ _SIGNATURES = {
     "gmlp_w4_matmul": ([_P] * 3 + [_I64, _I64, _I64, _INT, _INT, _INT, _P, _SZ, _P], _INT),
     "gmlp_w4_gate_up": ([_P] * 4 + [_I64, _I64, _I64, _INT, _INT, _INT, _F, _INT, _P, _SZ, _P], _INT),
     "gmlp_w4_forward": ([_P] * 5 + [_I64, _I64, _I64, _INT, _INT, _INT, _F, _INT, _P, _SZ, _P], _INT),
+    "gmlp_route_sort": ([_P] * 3 + [_I64, _I64, _I64, _INT, _P], _INT),
+    "gmlp_route_dispatch": ([_P] * 3 + [_I64, _I64, _I64, _P], _INT),
+    "gmlp_route_combine": ([_P] * 4 + [_I64, _I64, _I64, _INT, _P], _INT),
+    "gmlp_route_combine_backward": ([_P] * 6 + [_I64, _I64, _I64, _INT, _P], _INT),
+    "gmlp_dropout": ([_P] * 3 + [_I64, _I64, _D, _U64, _U64, _P, _INT, _P], _INT),
+    "gmlp_dropout_backward": ([_P] * 2 + [_I64, _I64, _D, _U64, _U64, _P, _INT, _P], _INT),
 }
 
 _lib = None

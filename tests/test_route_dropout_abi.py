@@ -1,0 +1,106 @@
+"""Host-side checks of the routing and dropout entry points (no GPU)."""
+import pytest
+
+from paper_2606_26344_amd import dropout, gmlp
+
+A = 0x10000000  # fake addresses: validation never dereferences
+MB = 1 << 20
+
+
+def call(name, *args):
+    return getattr(gmlp.library(), name)(*args, None)
+
+
+def sort(ids=A, offsets=A + MB, slots=A + 2 * MB, T=16, k=2, E=8, flags=0):
+    return call("gmlp_route_sort", ids, offsets, slots, T, k, E, flags)
+
+
+def dispatch(X=A, slots=A + 50 * MB, xs=A + 60 * MB, T=16, k=2, D=256):
+    return call("gmlp_route_dispatch", X, slots, xs, T, k, D)
+
+
+def combine(ys=A, slots=A + 50 * MB, weights=A + 51 * MB, Y=A + 60 * MB, T=16, k=2, D=256, flags=0):
+    return call("gmlp_route_combine", ys, slots, weights, Y, T, k, D, flags)
+
+
+def combine_backward(dY=A, ys=A + 10 * MB, slots=A + 50 * MB, weights=A + 51 * MB, dys=A + 60 * MB, dweights=A + 52 * MB,
+                     T=16, k=2, D=256, flags=0):
+    return call("gmlp_route_combine_backward", dY, ys, slots, weights, dys, dweights, T, k, D, flags)
+
+
+def drop(X=A, res=A + 10 * MB, out=A + 20 * MB, T=16, D=256, p=0.1, seed=1, offset=0, position=None, flags=0):
+    return call("gmlp_dropout", X, res, out, T, D, p, seed, offset, position, flags)
+
+
+def drop_backward(dout=A, dX=A + 20 * MB, T=16, D=256, p=0.1, seed=1, offset=0, position=None, flags=0):
+    return call("gmlp_dropout_backward", dout, dX, T, D, p, seed, offset, position, flags)
+
+
+def test_sort_refusals():
+    assert sort(T=-1) == 1 and sort(k=0) == 1 and sort(E=0) == 1 and sort(E=-3) == 1
+    assert sort(E=1025) == 2 and sort(k=65) == 2 and sort(T=1 << 24, k=2) == 2 and sort(T=1 << 62, k=2) == 2
+    assert sort(flags=4) == 1 and sort(flags=1) == 1
+    for name in ("ids", "offsets", "slots"):
+        assert sort(**{name: None}) == 1 and name in gmlp.last_error()
+        assert sort(**{name: A + 90 * MB + 2}) == 2 and name in gmlp.last_error()
+    assert sort(ids=A + 4, flags=2) == 2  # 64-bit ids
+    assert sort(offsets=A + 4) == 1 and sort(slots=A) == 1 and sort(slots=A + MB + 32) == 1
+
+
+@pytest.mark.parametrize("f", [dispatch, combine, combine_backward])
+def test_row_refusals(f):
+    assert f(T=-1) == 1 and f(k=0) == 1 and f(D=0) == 1 and f(D=260) == 2 and f(k=65) == 2
+    assert f(D=(1 << 22) + 8) == 2 and f(T=(1 << 24) + 1, k=1) == 2 and f(T=1 << 22, k=4, D=1 << 15) == 2
+    if f is not dispatch:
+        assert f(flags=2) == 1
+    rows = {dispatch: ("X", "xs"), combine: ("ys", "Y"), combine_backward: ("dY", "ys")}[f]
+    for name in rows:
+        assert f(**{name: None}) == 1 and name in gmlp.last_error()
+        assert f(**{name: A + 90 * MB + 8}) == 2 and name in gmlp.last_error()
+    assert f(slots=None) == 1 and f(slots=A + 50 * MB + 2) == 2
+    if f is not dispatch:
+        assert f(weights=A + 51 * MB + 2) == 2
+
+
+def test_row_overlaps():
+    assert dispatch(xs=A) == 1 and dispatch(xs=A + 8176) == 1 and dispatch(slots=A + 60 * MB) == 1
+    assert combine(Y=A + 256) == 1 and combine(Y=A + 51 * MB) == 1
+    assert combine_backward(dys=A) == 1 and combine_backward(dys=A + 10 * MB + 512) == 1
+    assert combine_backward(dweights=A + 60 * MB) == 1 and combine_backward(dweights=A + 50 * MB) == 1
+    assert combine_backward(weights=None) == 1
+
+
+def test_nothing_to_do():
+    for f in (dispatch, combine, combine_backward):
+        names = {dispatch: ("X", "slots", "xs"), combine: ("ys", "slots", "weights", "Y"),
+                 combine_backward: ("dY", "ys", "slots", "weights", "dys", "dweights")}[f]
+        assert f(T=0, **{n: None for n in names}) == 0
+    assert combine_backward(dys=None, dweights=None) == 0
+    assert drop(X=None, res=None, out=None, T=0) == 0 and drop_backward(None, None, T=0) == 0
+
+
+@pytest.mark.parametrize("f", [drop, drop_backward])
+def test_dropout_refusals(f):
+    assert f(T=-1) == 1 and f(D=0) == 1 and f(D=12) == 2 and f(D=(1 << 22) + 8) == 2 and f(T=(1 << 24) + 1) == 2
+    assert f(T=1 << 24, D=1 << 14) == 2
+    assert f(p=-0.1) == 1 and f(p=1.0001) == 1 and f(p=float("nan")) == 1 and f(flags=2) == 1
+    assert f(position=A + 90 * MB + 4) == 2
+    assert f(position=A + 20 * MB + 8) == 1  # inside of what is written
+    for name in ("X", "out") if f is drop else ("dout", "dX"):
+        assert f(**{name: None}) == 1 and name in gmlp.last_error()
+        assert f(**{name: A + 50 * MB + 8}) == 2 and name in gmlp.last_error()
+
+
+def test_dropout_overlaps():
+    assert drop(out=A + 16) == 1 and drop(out=A + 10 * MB - 16) == 1
+    assert drop(out=A, flags=1) == 1  # fp32 over bf16
+    assert drop(res=None, flags=1) == 1
+    assert drop_backward(dX=A, flags=1) == 1 and drop_backward(dX=A + 16) == 1
+
+
+def test_dropout_numbers():
+    assert dropout.counters(3, 264) == 99
+    for bad in (-1, 1 << 64, 0.5, "1"):
+        with pytest.raises(ValueError, match="seed"):
+            dropout._number(bad, "seed")
+    assert dropout._number((1 << 64) - 1, "seed") == (1 << 64) - 1
