@@ -12,7 +12,7 @@ without loading the GPU library.
 """
 import importlib
 
-__all__ = ["gmlp", "train", "block_norm", "w4", "route", "dropout", "inputs", "build"]
+__all__ = ["gmlp", "train", "block_norm", "w4", "route", "experts", "dropout", "inputs", "build"]
 
 
 def __getattr__(name):

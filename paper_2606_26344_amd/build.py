@@ -18,7 +18,8 @@ ROOT = os.path.dirname(PKG)
 CSRC = os.path.join(PKG, "csrc")
 INCLUDE = os.path.join(ROOT, "include")
 LIBRARY = os.path.join(PKG, "libgmlp.so")
-SOURCES = [os.path.join(CSRC, f) for f in ("gmlp.hip", "train.hip", "block_norm.hip", "w4.hip", "route.hip", "dropout.hip")]
+SOURCES = [os.path.join(CSRC, f) for f in ("gmlp.hip", "train.hip", "block_norm.hip", "w4.hip", "route.hip", "experts.hip",
+                                              "dropout.hip")]
 # A measuring program beside the library (not part of it): the board's
 # sustained bf16 matrix-core rate, which bench.py reports as context.
 MFMA_CEILING = os.path.join(PKG, "mfma_ceiling")
@@ -26,7 +27,7 @@ MFMA_CEILING_SOURCE = os.path.join(CSRC, "mfma_ceiling.hip")
 HEADERS = [os.path.join(CSRC, f) for f in sorted(os.listdir(CSRC)) if f.endswith(".hpp")] + [
     os.path.join(INCLUDE, h)
     for h in ("gmlp.h", "softmax_matmul.h", "gmlp_train.h", "gmlp_block_norm.h", "gmlp_w4.h", "gmlp_route.h",
-              "gmlp_dropout.h")]
+              "gmlp_experts.h", "gmlp_dropout.h")]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

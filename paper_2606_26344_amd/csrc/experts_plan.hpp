@@ -1,0 +1,229 @@
+// Host-side planning of the experts' matmuls (include/gmlp_experts.h): tile shapes,
+// launch grids and the workspace layout.  Plain C++ with no HIP dependency.
+//
+// How many rows each expert has is known on the device only, so a plan goes by the rows
+// N and the experts E of the call: the tiles by the rows of an expert where they are
+// spread evenly, the grids by the most tiles that any spread can have.
+#pragma once
+
+#include "gmlp_experts.h"
+#include "grad_plan.hpp"
+
+namespace gmlp {
+
+// Which matmul a launch is.
+enum GroupedOp {
+    GROUPED_GATE_UP = 0, // H from X and two weights
+    GROUPED_SAVE = 1,    // H, G and U
+    GROUPED_DOWN = 2,    // Y = H Wd
+    GROUPED_DH = 3,      // dG, dU and H from dY Wd^T
+    GROUPED_DX = 4,      // dG Wg^T + dU Wu^T
+    GROUPED_DW = 5,      // the weight gradients
+};
+
+namespace {
+
+// Tiles of the products with a weight, by their rows.  The gate/up ones hold 128
+// columns of each of the two weights, side by side.
+template <int ROWS>
+struct GroupedShape;
+template <>
+struct GroupedShape<32> {
+    using GateUp = GradShape<4, 1, 2, 1, 4, 64, 1>;
+    using Other = GradTall32;
+};
+template <>
+struct GroupedShape<64> {
+    using GateUp = GradShape<4, 1, 2, 2, 3, 64, 1>;
+    using Other = GradTall64;
+};
+template <>
+struct GroupedShape<128> {
+    using GateUp = GradShape<4, 2, 2, 2, 3, 64, 1>;
+    using Other = GradSmall;
+};
+template <>
+struct GroupedShape<256> {
+    using GateUp = GradShape<4, 2, 2, 4, 2, 64, 1>;
+    using Other = GradLarge;
+};
+
+template <GroupedOp OP, int ROWS>
+using GroupedTile = std::conditional_t<OP == GROUPED_GATE_UP || OP == GROUPED_SAVE, typename GroupedShape<ROWS>::GateUp,
+                                       typename GroupedShape<ROWS>::Other>;
+// Columns of one weight in a tile.
+template <GroupedOp OP, class S>
+constexpr int grouped_columns() { return OP == GROUPED_GATE_UP || OP == GROUPED_SAVE ? S::BM / 2 : S::BM; }
+
+struct GroupedStep {
+    int rows = 32; // of a tile (weight gradients: the tile, enum GradTile)
+    int nk = 0, kt_seg = 0;
+    int columns = 0;        // column tiles
+    int most_row_tiles = 0; // of all experts
+    int slots = 0;          // blocks that run at once
+    int most_splits = 1;
+    int64_t problem_tiles = 0; // weight gradients: tiles of one gradient of one expert
+    int64_t blocks = 0;
+    int threads = 0;
+    size_t partial_bytes = 0;
+};
+
+// f(integral_constant<rows>) of a tile.
+template <class F>
+auto with_grouped_rows(int rows, F f)
+{
+    using std::integral_constant;
+    switch (rows) {
+    case 32: return f(integral_constant<int, 32>{});
+    case 64: return f(integral_constant<int, 64>{});
+    case 128: return f(integral_constant<int, 128>{});
+    default: return f(integral_constant<int, 256>{});
+    }
+}
+
+// Rows of an expert where they are spread evenly over as many experts as can have some.
+inline double rows_per_expert(int64_t N, int64_t E) { return (double)N / (double)std::max<int64_t>(1, std::min(N, E)); }
+
+inline int grouped_tile_rows(int64_t N, int64_t E)
+{
+    const double n = rows_per_expert(N, E);
+    return n <= 24 ? 32 : n <= 48 ? 64 : n <= 160 ? 128 : 256;
+}
+
+// A product of M columns with `segments` contractions of K each, on tiles of ROWS rows.
+template <GroupedOp OP, int ROWS>
+GroupedStep grouped_step(int64_t N, int64_t E, int64_t M, int64_t K, int segments)
+{
+    using S = GroupedTile<OP, ROWS>;
+    GroupedStep s;
+    s.rows = ROWS;
+    s.kt_seg = (int)cdiv(K, S::BK);
+    s.nk = segments * s.kt_seg;
+    s.columns = (int)cdiv(M, grouped_columns<OP, S>());
+    // Every expert with rows has one tile that may not be full.
+    s.most_row_tiles = (int)std::min<int64_t>(N / ROWS + std::min(E, N), N);
+    s.slots = kBlockTarget * S::BLOCKS;
+    // Tiles that do not fill the chip are split over k: the count with the least of the
+    // k-tiles' time and that of the exchange, n x (as in split_time), if that gains.
+    const double per = grad_tile_time<S>(), bytes = (double)S::BM * S::BN * sizeof(float);
+    const double x = bytes / 54e3 + bytes * s.slots / 8e6 / 4;
+    const double whole = s.nk * per;
+    const int n = (int)std::min(std::sqrt(whole / x), (double)std::max(1, s.nk / 2));
+    s.most_splits = n >= 2 && whole - whole / n > 4.0 + n * x ? n : 1;
+    s.blocks = (int64_t)s.most_row_tiles * s.columns;
+    if (s.most_splits > 1)
+        s.blocks = s.blocks / s.slots * s.slots + s.slots;
+    s.threads = S::NTHREADS;
+    s.partial_bytes = s.most_splits > 1 ? (size_t)s.slots * S::BM * S::BN * sizeof(float) : 0;
+    return s;
+}
+
+template <GroupedOp OP>
+GroupedStep grouped_step(int64_t N, int64_t E, int64_t M, int64_t K, int segments = 1)
+{
+    return with_grouped_rows(grouped_tile_rows(N, E),
+                             [&](auto rows) { return grouped_step<OP, decltype(rows)::value>(N, E, M, K, segments); });
+}
+
+// Tiles of the weight gradients, by the rows of an expert (measured for one expert, see
+// grad_plan.hpp).
+inline GradTile grouped_weight_tile(int64_t N, int64_t E, int64_t D, int64_t F)
+{
+    const double n = rows_per_expert(N, E);
+    if (n <= 256 && 3 * E * cdiv(D, 128) * cdiv(F, 256) <= 2 * kBlockTarget)
+        return GRAD_SHORT;
+    return n <= 1536 ? GRAD_PAIR : GRAD_LARGE;
+}
+
+// f(GradShapeTag) of a tile of the weight gradients.
+template <class F>
+auto with_grouped_weight_tile(GradTile t, F f)
+{
+    switch (t) {
+    case GRAD_SHORT: return f(GradShapeTag<GradShort, GRAD_SHORT>{});
+    case GRAD_PAIR: return f(GradShapeTag<GradPair, GRAD_PAIR>{});
+    default: return f(GradShapeTag<GradLarge, GRAD_LARGE>{});
+    }
+}
+
+// `problems` of the three gradients; dWd is the transposed shape of the others.
+inline GroupedStep grouped_weight_step(int problems, int64_t N, int64_t E, int64_t D, int64_t F)
+{
+    GroupedStep s;
+    const GradTile t = grouped_weight_tile(N, E, D, F);
+    s.rows = t;
+    with_grouped_weight_tile(t, [&](auto tag) {
+        using S = typename decltype(tag)::type;
+        s.problem_tiles = std::max(cdiv(F, S::BM) * cdiv(D, S::BN), cdiv(D, S::BM) * cdiv(F, S::BN));
+        s.threads = S::NTHREADS;
+        return 0;
+    });
+    s.blocks = E * problems * s.problem_tiles;
+    return s;
+}
+
+struct GroupedPlan {
+    GroupedStep gate_up, save, down, dh, dx, dw;
+};
+
+inline GroupedPlan grouped_plan(int64_t N, int64_t E, int64_t D, int64_t F)
+{
+    GroupedPlan p;
+    const int64_t n = std::max<int64_t>(N, 1);
+    p.gate_up = grouped_step<GROUPED_GATE_UP>(n, E, F, D);
+    p.save = grouped_step<GROUPED_SAVE>(n, E, F, D);
+    p.down = grouped_step<GROUPED_DOWN>(n, E, D, F);
+    p.dh = grouped_step<GROUPED_DH>(n, E, F, D);
+    p.dx = grouped_step<GROUPED_DX>(n, E, D, F, 2);
+    p.dw = grouped_weight_step(3, N, E, D, F);
+    return p;
+}
+
+// The workspace: counters, H, dG and dU, the partial sums of one step.
+struct GroupedLayout {
+    size_t h_off = 0, dg_off = 0, du_off = 0, partial_off = 0, total = 0;
+    int counters = 0;
+};
+
+inline GroupedLayout grouped_layout(int64_t N, int64_t E, int64_t D, int64_t F)
+{
+    GroupedLayout l;
+    const size_t h = align_up((size_t)N * F * 2);
+    l.h_off = kCounterBytes;
+    l.dg_off = l.h_off + h;
+    l.du_off = l.dg_off + h;
+    l.partial_off = l.du_off + h;
+    // Fewer rows have smaller tiles, with fewer sums; those of any tile up to this
+    // call's are provided for.
+    size_t partial = 0;
+    for (int64_t n : {N, std::min(N, 160 * E), std::min(N, 48 * E), std::min(N, 24 * E)}) {
+        const GroupedPlan p = grouped_plan(n, E, D, F);
+        partial = std::max({partial, p.gate_up.partial_bytes, p.save.partial_bytes, p.down.partial_bytes, p.dh.partial_bytes,
+                            p.dx.partial_bytes});
+    }
+    l.total = l.partial_off + align_up(partial);
+    l.counters = 2 * kBlockTarget; // of the tiles that are split: at most as many as run at once
+    return l;
+}
+
+inline int check_experts_shape(int64_t N, int64_t E, int64_t D, int64_t F)
+{
+    if (N < 0 || E <= 0 || D <= 0 || F <= 0)
+        return fail(GMLP_ERR_INVALID_ARG, "invalid shape N=%lld E=%lld D=%lld F=%lld (need N >= 0, the others > 0)",
+                    (long long)N, (long long)E, (long long)D, (long long)F);
+    if (D % 8 || F % 8)
+        return fail(GMLP_ERR_UNSUPPORTED, "D=%lld and F=%lld must be multiples of 8", (long long)D, (long long)F);
+    if (E > GMLP_MAX_EXPERTS || D > GMLP_EXPERTS_MAX_WIDTH || F > GMLP_EXPERTS_MAX_WIDTH || N > kMaxTokens ||
+        E * D * F > kMaxElements || N * std::max(D, F) > kMaxElements)
+        return fail(GMLP_ERR_UNSUPPORTED, "shape N=%lld E=%lld D=%lld F=%lld exceeds the supported range (E <= %d, D, F <= %d, "
+                    "N <= %lld, at most %lld elements per tensor)", (long long)N, (long long)E, (long long)D, (long long)F,
+                    GMLP_MAX_EXPERTS, GMLP_EXPERTS_MAX_WIDTH, (long long)kMaxTokens, (long long)kMaxElements);
+    const GroupedPlan p = grouped_plan(N, E, D, F);
+    for (const GroupedStep *s : {&p.gate_up, &p.down, &p.dh, &p.dx, &p.dw})
+        if (s->blocks * s->threads >= (int64_t(1) << 32) || s->blocks >= (int64_t(1) << 31))
+            return fail(GMLP_ERR_UNSUPPORTED, "%lld blocks exceed a launch grid", (long long)s->blocks);
+    return GMLP_OK;
+}
+
+} // namespace
+} // namespace gmlp

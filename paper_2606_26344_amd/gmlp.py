@@ -35,7 +35,7 @@ LIBRARY = os.path.join(HERE, "libgmlp.so")
 HEADER = os.path.join(os.path.dirname(HERE), "include", "gmlp.h")
 HEADERS = [os.path.join(os.path.dirname(HERE), "include", h)
            for h in ("gmlp.h", "softmax_matmul.h", "gmlp_train.h", "gmlp_block_norm.h", "gmlp_w4.h",
-                     "gmlp_route.h", "gmlp_dropout.h")]
+                     "gmlp_route.h", "gmlp_experts.h", "gmlp_dropout.h")]
 
 PATH_AUTO, PATH_GEMV, PATH_MFMA, PATH_FUSED, PATH_FUSED_MFMA = 0, 1, 2, 3, 4
 _PATHS = {"auto": PATH_AUTO, "gemv": PATH_GEMV, "mfma": PATH_MFMA, "fused": PATH_FUSED,
@@ -102,6 +102,10 @@ _SIGNATURES = {
     "gmlp_route_dispatch": ([_P] * 3 + [_I64, _I64, _I64, _P], _INT),
     "gmlp_route_combine": ([_P] * 4 + [_I64, _I64, _I64, _INT, _P], _INT),
     "gmlp_route_combine_backward": ([_P] * 6 + [_I64, _I64, _I64, _INT, _P], _INT),
+    "gmlp_experts_workspace_size": ([_I64] * 4, _SZ),
+    "gmlp_experts_describe": ([_I64] * 4 + [_INT, ctypes.c_char_p, _SZ], _INT),
+    "gmlp_experts_forward": ([_P] * 8 + [_I64] * 4 + [_INT, _F, _INT, _P, _SZ, _P], _INT),
+    "gmlp_experts_backward": ([_P] * 12 + [_I64] * 4 + [_INT, _F, _INT, _P, _SZ, _P], _INT),
     "gmlp_dropout": ([_P] * 3 + [_I64, _I64, _D, _U64, _U64, _P, _INT, _P], _INT),
     "gmlp_dropout_backward": ([_P] * 2 + [_I64, _I64, _D, _U64, _U64, _P, _INT, _P], _INT),
 }
