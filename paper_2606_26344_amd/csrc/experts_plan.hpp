@@ -158,7 +158,7 @@ inline GroupedStep grouped_weight_step(int problems, int64_t N, int64_t E, int64
         s.threads = S::NTHREADS;
         return 0;
     });
-    s.blocks = E * problems * s.problem_tiles;
+    s.blocks = E * (cdiv(problems * s.problem_tiles, 8) * 8);
     return s;
 }
 

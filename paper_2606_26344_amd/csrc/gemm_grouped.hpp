@@ -141,11 +141,16 @@ __global__ __launch_bounds__(S::NTHREADS, S::BLOCKS) void gemm_grouped_kernel(Gr
     int kt_begin = 0, kt_end, splits = 1, split = 0, piece_tile = 0, rest = 0;
     bool whole = true;
     if constexpr (WEIGHTS) {
-        const int tile = xcd_contiguous_id(bid, p.experts * p.problems * p.problem_tiles);
-        const int per = p.problems * p.problem_tiles;
-        expert = tile / per;
-        prob = (tile - expert * per) / p.problem_tiles;
-        local = tile - expert * per - prob * p.problem_tiles;
+        // Every XCD takes an eighth of each expert's tiles, since experts have more or
+        // less to contract: with whole experts by XCD the one with the most rows kept
+        // the others waiting (8 experts of 558 to 1879 rows, 4096 x 14336: 4350 us).
+        const int per = p.problems * p.problem_tiles, padded = (per + 7) / 8 * 8;
+        expert = bid / padded;
+        if (bid - expert * padded >= per)
+            return;
+        const int tile = xcd_contiguous_id(bid - expert * padded, per);
+        prob = tile / p.problem_tiles;
+        local = tile - prob * p.problem_tiles;
         first = count = 0;
         if (p.rows > 0) // else there may be no offsets
             expert_rows(p, expert, first, count);
@@ -194,302 +199,324 @@ __global__ __launch_bounds__(S::NTHREADS, S::BLOCKS) void gemm_grouped_kernel(Gr
     const int group_w = min(tiles_m - group * 8, 8);
     const int m0 = (group * 8 + in_group % group_w) * BMW, n0 = (in_group / group_w) * S::BN;
 
-    // Operands and outputs of this expert: the weights by expert, the rows from its first.
-    const size_t a_at = WEIGHTS ? (size_t)first * M : (size_t)expert * M * K;
-    const size_t b_at = WEIGHTS ? (size_t)first * N : (size_t)first * K;
-    const size_t out_at = WEIGHTS ? (size_t)expert * M * N : (size_t)first * M;
-    GradLoader<KCA, BMW, S::NWAVES, BK> la;
-    GradLoader<KCB, S::BN, S::NWAVES, BK> lb;
-    la.init(m0, M, KCA ? K : M, wave, lane);
-    lb.init(n0, N, KCB ? K : N, wave, lane);
-    // Past the end zeros are read, so that every step has the same number of loads
-    // in flight.
-    int load_kt = kt_begin;
-    auto issue = [&](uint8_t *buf) __attribute__((always_inline)) {
-        const int seg = SEGS == 2 && load_kt >= p.kt_seg ? 1 : 0;
-        const int k0 = load_kt < kt_end ? (load_kt - seg * p.kt_seg) * BK : 0;
-        const int krem = load_kt < kt_end ? K - k0 : 0;
-        const int q = SEGS == 2 ? seg : prob;
-        la.issue(p.a[q] + a_at, k0, krem, buf, wave, lane);
-        if constexpr (NW == 2)
-            la.issue(p.a[1] + a_at, k0, krem, buf + S::A_BYTES / 2, wave, lane);
-        lb.issue(p.b[q] + b_at, k0, krem, buf + S::A_BYTES, wave, lane);
-        ++load_kt;
-    };
+    // The tile with TX of its TN row blocks per wave.
+    const int own_lane = lane;
+    auto run = [&]<int TX>() __attribute__((always_inline)) {
+        // Opaque, so that no address of one TX is computed ahead of the choice between
+        // them and kept in registers.
+        int lane = own_lane;
+        asm volatile("" : "+v"(lane));
+        constexpr int BX = S::WN * TX * 32, PIECES = TM * TX * 4;
+        constexpr int LOADS = (S::A_BYTES + BX * BK * 2) / (S::NTHREADS * 16);
+        // Operands and outputs of this expert: the weights by expert, the rows from its first.
+        const size_t a_at = WEIGHTS ? (size_t)first * M : (size_t)expert * M * K;
+        const size_t b_at = WEIGHTS ? (size_t)first * N : (size_t)first * K;
+        const size_t out_at = WEIGHTS ? (size_t)expert * M * N : (size_t)first * M;
+        GradLoader<KCA, BMW, S::NWAVES, BK> la;
+        GradLoader<KCB, BX, S::NWAVES, BK> lb;
+        la.init(m0, M, KCA ? K : M, wave, lane);
+        lb.init(n0, N, KCB ? K : N, wave, lane);
+        // Past the end zeros are read, so that every step has the same number of loads
+        // in flight.
+        int load_kt = kt_begin;
+        auto issue = [&](uint8_t *buf) __attribute__((always_inline)) {
+            const int seg = SEGS == 2 && load_kt >= p.kt_seg ? 1 : 0;
+            const int k0 = load_kt < kt_end ? (load_kt - seg * p.kt_seg) * BK : 0;
+            const int krem = load_kt < kt_end ? K - k0 : 0;
+            const int q = SEGS == 2 ? seg : prob;
+            la.issue(p.a[q] + a_at, k0, krem, buf, wave, lane);
+            if constexpr (NW == 2)
+                la.issue(p.a[1] + a_at, k0, krem, buf + S::A_BYTES / 2, wave, lane);
+            lb.issue(p.b[q] + b_at, k0, krem, buf + S::A_BYTES, wave, lane);
+            ++load_kt;
+        };
 
-    GradFragments<KCA, BMW, BK> qa;
-    GradFragments<KCB, S::BN, BK> qb;
-    qa.init(wm * TMW * 32, lane);
-    qb.init(wn * TN * 32, lane);
-    // Fragment q of the wave's A rows: those of the second weight behind the first's.
-    auto read_a = [&](const uint8_t *buf, int kk, int q) __attribute__((always_inline)) {
-        return qa.read(buf + (q / (2 * TMW)) * (S::A_BYTES / 2), kk, q % (2 * TMW));
-    };
+        GradFragments<KCA, BMW, BK> qa;
+        GradFragments<KCB, BX, BK> qb;
+        qa.init(wm * TMW * 32, lane);
+        qb.init(wn * TX * 32, lane);
+        // Fragment q of the wave's A rows: those of the second weight behind the first's.
+        auto read_a = [&](const uint8_t *buf, int kk, int q) __attribute__((always_inline)) {
+            return qa.read(buf + (q / (2 * TMW)) * (S::A_BYTES / 2), kk, q % (2 * TMW));
+        };
 
-    using Acc = AccBlock<true>;
-    Acc acc[TM][TN];
+        using Acc = AccBlock<true>;
+        Acc acc[TM][TX];
 #pragma unroll
-    for (int mi = 0; mi < TM; ++mi)
+        for (int mi = 0; mi < TM; ++mi)
 #pragma unroll
-        for (int ni = 0; ni < TN; ++ni)
+            for (int ni = 0; ni < TX; ++ni)
 #pragma unroll
-            for (int j = 0; j < 4; ++j)
-                acc[mi][ni].set_piece(j, f32x4{});
+                for (int j = 0; j < 4; ++j)
+                    acc[mi][ni].set_piece(j, f32x4{});
 
-    // The MFMAs of one k32 step, one group per 16-row B fragment, with the next
-    // step's fragment reads among them (as gemm_grad.hpp).
-    struct FragA {
-        bf16x8 a[TM * 2];
-    };
-    FragA fa0, fa1;
-    bf16x8 fb[TN * 2];
-    auto mma_roll = [&](const FragA &fa, FragA &fa_next, const uint8_t *nbuf, int nkk) __attribute__((always_inline)) {
-        constexpr int GROUPS = TN * 2, AFRAGS = TM * 2, APG = (AFRAGS + GROUPS - 1) / GROUPS;
-        [&]<int... G>(std::integer_sequence<int, G...>) __attribute__((always_inline)) {
-            (
-                [&] {
+        // The MFMAs of one k32 step, one group per 16-row B fragment, with the next
+        // step's fragment reads among them (as gemm_grad.hpp).
+        struct FragA {
+            bf16x8 a[TM * 2];
+        };
+        FragA fa0, fa1;
+        bf16x8 fb[TX * 2];
+        auto mma_roll = [&](const FragA &fa, FragA &fa_next, const uint8_t *nbuf, int nkk) __attribute__((always_inline)) {
+            constexpr int GROUPS = TX * 2, AFRAGS = TM * 2, APG = (AFRAGS + GROUPS - 1) / GROUPS;
+            [&]<int... G>(std::integer_sequence<int, G...>) __attribute__((always_inline)) {
+                (
+                    [&] {
 #pragma unroll
-                    for (int a = 0; a < AFRAGS; ++a)
-                        acc[a / 2][G / 2].v[a % 2 + 2 * (G % 2)] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                            fa.a[a], fb[G], acc[a / 2][G / 2].v[a % 2 + 2 * (G % 2)], 0, 0, 0);
+                        for (int a = 0; a < AFRAGS; ++a)
+                            acc[a / 2][G / 2].v[a % 2 + 2 * (G % 2)] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                                fa.a[a], fb[G], acc[a / 2][G / 2].v[a % 2 + 2 * (G % 2)], 0, 0, 0);
 #pragma unroll
-                    for (int q = G * APG; q < (G + 1) * APG && q < AFRAGS; ++q)
-                        fa_next.a[q] = read_a(nbuf, nkk, q);
-                    fb[G] = qb.read(nbuf + S::A_BYTES, nkk, G);
-                    __builtin_amdgcn_sched_barrier(0);
-                }(),
-                ...);
-        }(std::make_integer_sequence<int, GROUPS>{});
-    };
-    auto wait_tile = [&]() __attribute__((always_inline)) {
-        wait_vmcnt<(STAGES - 2) * S::LOADS_PER_STAGE>();
-        wait_lgkm0();
-        barrier_only();
-    };
+                        for (int q = G * APG; q < (G + 1) * APG && q < AFRAGS; ++q)
+                            fa_next.a[q] = read_a(nbuf, nkk, q);
+                        fb[G] = qb.read(nbuf + S::A_BYTES, nkk, G);
+                        __builtin_amdgcn_sched_barrier(0);
+                    }(),
+                    ...);
+            }(std::make_integer_sequence<int, GROUPS>{});
+        };
+        auto wait_tile = [&]() __attribute__((always_inline)) {
+            wait_vmcnt<(STAGES - 2) * LOADS>();
+            wait_lgkm0();
+            barrier_only();
+        };
 
-    [&]<int... I>(std::integer_sequence<int, I...>) __attribute__((always_inline)) {
-        (issue(stage_ptr(std::integral_constant<int, I>{})), ...);
-    }(std::make_integer_sequence<int, STAGES - 1>{});
-    wait_tile();
-    issue(stage_ptr(std::integral_constant<int, STAGES - 1>{}));
-#pragma unroll
-    for (int q = 0; q < TM * 2; ++q)
-        fa0.a[q] = read_a(lds0, 0, q);
-#pragma unroll
-    for (int q = 0; q < TN * 2; ++q)
-        fb[q] = qb.read(lds0 + S::A_BYTES, 0, q);
-    // The k-tile in stage I % STAGES.  At its last k32 step, whose fragments have
-    // been read, a barrier frees the stage for the DMA of the k-tile STAGES ahead
-    // and the next k-tile's first fragments are read.
-    auto step = [&](auto index) __attribute__((always_inline)) {
-        constexpr int I = decltype(index)::value;
-        uint8_t *buf = stage_ptr(std::integral_constant<int, I % STAGES>{});
-        uint8_t *next = stage_ptr(std::integral_constant<int, (I + 1) % STAGES>{});
-        if constexpr (BK == 64)
-            mma_roll(fa0, fa1, buf, 1);
-        wait_tile();
-        issue(buf);
-        if constexpr (BK == 64 || I % 2 == 1)
-            mma_roll(fa1, fa0, next, 0);
-        else
-            mma_roll(fa0, fa1, next, 0);
-    };
-    // A round of steps brings stages and fragment buffers back to the first.
-    constexpr int ROUND = BK == 64 || STAGES % 2 == 0 ? STAGES : 2 * STAGES;
-    int i = 0;
-    for (; i + ROUND <= nk; i += ROUND) {
         [&]<int... I>(std::integer_sequence<int, I...>) __attribute__((always_inline)) {
-            (step(std::integral_constant<int, I>{}), ...);
-        }(std::make_integer_sequence<int, ROUND>{});
-    }
-    [&]<int... I>(std::integer_sequence<int, I...>) __attribute__((always_inline)) {
-        ((i + I < nk ? step(std::integral_constant<int, I>{}) : void()), ...);
-    }(std::make_integer_sequence<int, ROUND - 1>{});
-    wait_vmcnt<0>(); // loads past the end, before LDS is given to another block
-
-    // ---- outputs ---------------------------------------------------------------
-    // A batch is the wave's 16 output rows of one B fragment: TM runs of 32 columns,
-    // eight of them per lane.  Batch b is half b % 2 of acc[.][b / 2].
-    constexpr int BATCHES = TN * 2;
-    const auto corner = [&](const uint16_t *t, bool used) __attribute__((always_inline)) {
-        return make_rsrc(used ? t + out_at + (size_t)n0 * M + m0 : nullptr);
-    };
-    constexpr bool DH = OP == GROUPED_DH, SAVE = OP == GROUPED_SAVE;
-    const __amdgpu_buffer_rsrc_t ro = corner(p.out[prob], !DH);
-    const __amdgpu_buffer_rsrc_t rg = corner(DH ? p.g : p.out[1], DH || SAVE), ru = corner(DH ? p.u : p.out[2], DH || SAVE);
-    const __amdgpu_buffer_rsrc_t rdg = corner(p.dg, DH), rdu = corner(p.du, DH), rh = corner(p.h, DH);
-    auto offset = [&](int b, int mi) __attribute__((always_inline)) {
-        const int ml = wm * TMW * 32 + mi * 32 + wide_column(lane), nl = wn * TN * 32 + b * 16 + (lane & 15);
-        const int in = (int)(n0 + nl < N) & (int)(m0 + ml < M); // without a branch
-        return in ? ((uint32_t)nl * (uint32_t)M + (uint32_t)ml) * 2u : kOutOfRange;
-    };
-    // Of a pair of runs: store `half` takes eight rows of 128 bytes (store_lines).
-    auto line_offset = [&](int b, int mi, int half) __attribute__((always_inline)) {
-        const int ml = wm * TM * 32 + mi * 32 + wide_column(lane) + 4 * (lane & 8);
-        const int nl = wn * TN * 32 + b * 16 + 8 * half + (lane & 7);
-        const int in = (int)(n0 + nl < N) & (int)(m0 + ml < M);
-        return in ? ((uint32_t)nl * (uint32_t)M + (uint32_t)ml) * 2u : kOutOfRange;
-    };
-    struct Gates {
-        u32x4 g[TM], u[TM];
-    };
-    // G and U of the batches ahead are on their way while one is computed.
-    constexpr int AHEAD = DH ? (BATCHES < 4 ? BATCHES : 4) : 1;
-    Gates gates[AHEAD];
-    auto load_gates = [&](Gates &v, int b) __attribute__((always_inline)) {
+            (issue(stage_ptr(std::integral_constant<int, I>{})), ...);
+        }(std::make_integer_sequence<int, STAGES - 1>{});
+        wait_tile();
+        issue(stage_ptr(std::integral_constant<int, STAGES - 1>{}));
 #pragma unroll
-        for (int mi = 0; mi < TM; ++mi) {
-            v.g[mi] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rg, offset(b, mi), 0, 0));
-            v.u[mi] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(ru, offset(b, mi), 0, 0));
+        for (int q = 0; q < TM * 2; ++q)
+            fa0.a[q] = read_a(lds0, 0, q);
+#pragma unroll
+        for (int q = 0; q < TX * 2; ++q)
+            fb[q] = qb.read(lds0 + S::A_BYTES, 0, q);
+        // The k-tile in stage I % STAGES.  At its last k32 step, whose fragments have
+        // been read, a barrier frees the stage for the DMA of the k-tile STAGES ahead
+        // and the next k-tile's first fragments are read.
+        auto step = [&](auto index) __attribute__((always_inline)) {
+            constexpr int I = decltype(index)::value;
+            uint8_t *buf = stage_ptr(std::integral_constant<int, I % STAGES>{});
+            uint8_t *next = stage_ptr(std::integral_constant<int, (I + 1) % STAGES>{});
+            if constexpr (BK == 64)
+                mma_roll(fa0, fa1, buf, 1);
+            wait_tile();
+            issue(buf);
+            if constexpr (BK == 64 || I % 2 == 1)
+                mma_roll(fa1, fa0, next, 0);
+            else
+                mma_roll(fa0, fa1, next, 0);
+        };
+        // A round of steps brings stages and fragment buffers back to the first.
+        constexpr int ROUND = BK == 64 || STAGES % 2 == 0 ? STAGES : 2 * STAGES;
+        int i = 0;
+        for (; i + ROUND <= nk; i += ROUND) {
+            [&]<int... I>(std::integer_sequence<int, I...>) __attribute__((always_inline)) {
+                (step(std::integral_constant<int, I>{}), ...);
+            }(std::make_integer_sequence<int, ROUND>{});
         }
-    };
-    auto pack8 = [](const float (&v)[8]) __attribute__((always_inline)) {
-        return u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
-    };
-    // lo, hi: the two MFMA results of each run.
-    auto emit = [&](int b, const f32x4 (&lo)[TM], const f32x4 (&hi)[TM]) __attribute__((always_inline)) {
-        if constexpr (GATE_UP) {
-#pragma unroll
-            for (int mi = 0; mi < TMW; ++mi) {
-                float g[8], u[8], h[8];
-                wide_columns(lo[mi], hi[mi], g);
-                wide_columns(lo[TMW + mi], hi[TMW + mi], u);
-#pragma unroll
-                for (int e = 0; e < 8; ++e)
-                    h[e] = gate_act(g[e], p.activation, p.beta) * u[e];
-                const uint32_t off = offset(b, mi);
-                if constexpr (SAVE) {
-                    __builtin_amdgcn_raw_buffer_store_b128(pack8(g), rg, off, 0, 0);
-                    __builtin_amdgcn_raw_buffer_store_b128(pack8(u), ru, off, 0, 0);
-                }
-                __builtin_amdgcn_raw_buffer_store_b128(pack8(h), ro, off, 0, 0);
-            }
-        } else {
-            u32x4 c[TM];
+        [&]<int... I>(std::integer_sequence<int, I...>) __attribute__((always_inline)) {
+            ((i + I < nk ? step(std::integral_constant<int, I>{}) : void()), ...);
+        }(std::make_integer_sequence<int, ROUND - 1>{});
+        wait_vmcnt<0>(); // loads past the end, before LDS is given to another block
+        asm volatile("" : "+v"(lane)); // the outputs' addresses are made here, not before the loop
+
+        // ---- outputs ---------------------------------------------------------------
+        // A batch is the wave's 16 output rows of one B fragment: TM runs of 32 columns,
+        // eight of them per lane.  Batch b is half b % 2 of acc[.][b / 2].
+        constexpr int BATCHES = TX * 2;
+        const auto corner = [&](const uint16_t *t, bool used) __attribute__((always_inline)) {
+            return make_rsrc(used ? t + out_at + (size_t)n0 * M + m0 : nullptr);
+        };
+        constexpr bool DH = OP == GROUPED_DH, SAVE = OP == GROUPED_SAVE;
+        const __amdgpu_buffer_rsrc_t ro = corner(p.out[prob], !DH);
+        const __amdgpu_buffer_rsrc_t rg = corner(DH ? p.g : p.out[1], DH || SAVE), ru = corner(DH ? p.u : p.out[2], DH || SAVE);
+        const __amdgpu_buffer_rsrc_t rdg = corner(p.dg, DH), rdu = corner(p.du, DH), rh = corner(p.h, DH);
+        auto offset = [&](int b, int mi) __attribute__((always_inline)) {
+            const int ml = wm * TMW * 32 + mi * 32 + wide_column(lane), nl = wn * TX * 32 + b * 16 + (lane & 15);
+            const int in = (int)(n0 + nl < N) & (int)(m0 + ml < M); // without a branch
+            return in ? ((uint32_t)nl * (uint32_t)M + (uint32_t)ml) * 2u : kOutOfRange;
+        };
+        // Of a pair of runs: store `half` takes eight rows of 128 bytes (store_lines).
+        auto line_offset = [&](int b, int mi, int half) __attribute__((always_inline)) {
+            const int ml = wm * TM * 32 + mi * 32 + wide_column(lane) + 4 * (lane & 8);
+            const int nl = wn * TX * 32 + b * 16 + 8 * half + (lane & 7);
+            const int in = (int)(n0 + nl < N) & (int)(m0 + ml < M);
+            return in ? ((uint32_t)nl * (uint32_t)M + (uint32_t)ml) * 2u : kOutOfRange;
+        };
+        struct Gates {
+            u32x4 g[TM], u[TM];
+        };
+        // G and U of the batches ahead are on their way while one is computed.
+        constexpr int AHEAD = DH ? (BATCHES < 4 ? BATCHES : 4) : 1;
+        Gates gates[AHEAD];
+        auto load_gates = [&](Gates &v, int b) __attribute__((always_inline)) {
 #pragma unroll
             for (int mi = 0; mi < TM; ++mi) {
-                float v[8];
-                wide_columns(lo[mi], hi[mi], v);
-                if constexpr (DH) {
+                v.g[mi] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(rg, offset(b, mi), 0, 0));
+                v.u[mi] = __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(ru, offset(b, mi), 0, 0));
+            }
+        };
+        auto pack8 = [](const float (&v)[8]) __attribute__((always_inline)) {
+            return u32x4{pack_bf16x2(v[0], v[1]), pack_bf16x2(v[2], v[3]), pack_bf16x2(v[4], v[5]), pack_bf16x2(v[6], v[7])};
+        };
+        // lo, hi: the two MFMA results of each run.
+        auto emit = [&](int b, const f32x4 (&lo)[TM], const f32x4 (&hi)[TM]) __attribute__((always_inline)) {
+            if constexpr (GATE_UP) {
+#pragma unroll
+                for (int mi = 0; mi < TMW; ++mi) {
+                    float g[8], u[8], h[8];
+                    wide_columns(lo[mi], hi[mi], g);
+                    wide_columns(lo[TMW + mi], hi[TMW + mi], u);
+#pragma unroll
+                    for (int e = 0; e < 8; ++e)
+                        h[e] = gate_act(g[e], p.activation, p.beta) * u[e];
                     const uint32_t off = offset(b, mi);
-                    const Gates &gu = gates[b % AHEAD];
-                    u32x4 dg, du, h;
-                    gate_gradients(v, gu.g[mi], gu.u[mi], p.activation, p.beta, dg, du, h);
-                    __builtin_amdgcn_raw_buffer_store_b128(dg, rdg, off, 0, 0);
-                    __builtin_amdgcn_raw_buffer_store_b128(du, rdu, off, 0, 0);
-                    __builtin_amdgcn_raw_buffer_store_b128(h, rh, off, 0, 0);
-                } else {
-                    c[mi] = pack8(v);
+                    if constexpr (SAVE) {
+                        __builtin_amdgcn_raw_buffer_store_b128(pack8(g), rg, off, 0, 0);
+                        __builtin_amdgcn_raw_buffer_store_b128(pack8(u), ru, off, 0, 0);
+                    }
+                    __builtin_amdgcn_raw_buffer_store_b128(pack8(h), ro, off, 0, 0);
+                }
+            } else {
+                u32x4 c[TM];
+#pragma unroll
+                for (int mi = 0; mi < TM; ++mi) {
+                    float v[8];
+                    wide_columns(lo[mi], hi[mi], v);
+                    if constexpr (DH) {
+                        const uint32_t off = offset(b, mi);
+                        const Gates &gu = gates[b % AHEAD];
+                        u32x4 dg, du, h;
+                        gate_gradients(v, gu.g[mi], gu.u[mi], p.activation, p.beta, dg, du, h);
+                        __builtin_amdgcn_raw_buffer_store_b128(dg, rdg, off, 0, 0);
+                        __builtin_amdgcn_raw_buffer_store_b128(du, rdu, off, 0, 0);
+                        __builtin_amdgcn_raw_buffer_store_b128(h, rh, off, 0, 0);
+                    } else {
+                        c[mi] = pack8(v);
+                    }
+                }
+                if constexpr (!DH && TM % 2 == 0) {
+#pragma unroll
+                    for (int mi = 0; mi < TM; mi += 2) {
+                        store_lines(c[mi], c[mi + 1], lane);
+#pragma unroll
+                        for (int half = 0; half < 2; ++half)
+                            __builtin_amdgcn_raw_buffer_store_b128(c[mi + half], ro, line_offset(b, mi, half), 0, OUT_POLICY);
+                    }
+                } else if constexpr (!DH) {
+#pragma unroll
+                    for (int mi = 0; mi < TM; ++mi)
+                        __builtin_amdgcn_raw_buffer_store_b128(c[mi], ro, offset(b, mi), 0, OUT_POLICY);
                 }
             }
-            if constexpr (!DH && TM % 2 == 0) {
+            if constexpr (DH)
+                if (b + AHEAD < BATCHES)
+                    load_gates(gates[b % AHEAD], b + AHEAD);
+            __builtin_amdgcn_sched_barrier(0);
+        };
+        auto piece = [&](int b, int mi, int sa) __attribute__((always_inline)) { return acc[mi][b / 2].v[sa + 2 * (b % 2)]; };
+        auto first_gates = [&]() __attribute__((always_inline)) {
+            if constexpr (DH)
 #pragma unroll
-                for (int mi = 0; mi < TM; mi += 2) {
-                    store_lines(c[mi], c[mi + 1], lane);
-#pragma unroll
-                    for (int half = 0; half < 2; ++half)
-                        __builtin_amdgcn_raw_buffer_store_b128(c[mi + half], ro, line_offset(b, mi, half), 0, OUT_POLICY);
-                }
-            } else if constexpr (!DH) {
-#pragma unroll
-                for (int mi = 0; mi < TM; ++mi)
-                    __builtin_amdgcn_raw_buffer_store_b128(c[mi], ro, offset(b, mi), 0, OUT_POLICY);
-            }
-        }
-        if constexpr (DH)
-            if (b + AHEAD < BATCHES)
-                load_gates(gates[b % AHEAD], b + AHEAD);
-        __builtin_amdgcn_sched_barrier(0);
-    };
-    auto piece = [&](int b, int mi, int sa) __attribute__((always_inline)) { return acc[mi][b / 2].v[sa + 2 * (b % 2)]; };
-    auto first_gates = [&]() __attribute__((always_inline)) {
-        if constexpr (DH)
-#pragma unroll
-            for (int b = 0; b < AHEAD; ++b)
-                load_gates(gates[b], b);
-    };
+                for (int b = 0; b < AHEAD; ++b)
+                    load_gates(gates[b], b);
+        };
 
-    if constexpr (!WEIGHTS) {
-        if (splits > 1 && !whole) {
-            // Partial sums out with device-coherent stores, [split][tile][wave]
-            // [batch][piece][lane]; the last block of a tile reads them all back and
-            // adds them in the order of the splits, whichever block it is.
-            const __amdgpu_buffer_rsrc_t prs = make_rsrc(p.partial);
-            const uint32_t lane_off = lane * 16;
-            auto wave_base = [&](int sp) __attribute__((always_inline)) {
-                return (uint32_t)(((sp * rest + piece_tile) * S::NWAVES + wave) * S::PIECES) * 1024u;
-            };
-            const uint32_t own = wave_base(split);
+        if constexpr (!WEIGHTS) {
+            if (splits > 1 && !whole) {
+                // Partial sums out with device-coherent stores, [split][tile][wave]
+                // [batch][piece][lane]; the last block of a tile reads them all back and
+                // adds them in the order of the splits, whichever block it is.
+                const __amdgpu_buffer_rsrc_t prs = make_rsrc(p.partial);
+                const uint32_t lane_off = lane * 16;
+                auto wave_base = [&](int sp) __attribute__((always_inline)) {
+                    return (uint32_t)(((sp * rest + piece_tile) * S::NWAVES + wave) * S::PIECES) * 1024u; // tiles of any TX side by side
+                };
+                const uint32_t own = wave_base(split);
 #pragma unroll
-            for (int b = 0; b < BATCHES; ++b)
+                for (int b = 0; b < BATCHES; ++b)
 #pragma unroll
-                for (int mi = 0; mi < TM; ++mi)
-#pragma unroll
-                    for (int sa = 0; sa < 2; ++sa)
-                        __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, piece(b, mi, sa)), prs, lane_off,
-                                                               own + ((b * TM + mi) * 2 + sa) * 1024u, kCoherent);
-            wait_vmcnt<0>();
-            __syncthreads();
-            if (tid == 0) {
-                const uint32_t before =
-                    __hip_atomic_fetch_add(p.counters + piece_tile, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-                s_last = before == (uint32_t)(splits - 1);
-            }
-            __syncthreads();
-            if (!s_last)
-                return;
-            if (tid == 0)
-                __hip_atomic_store(p.counters + piece_tile, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
-            first_gates();
-            // GROUP batches' sums at once: the loads of one split, of up to 20 pieces, are
-            // in flight together, and each split costs their latency for every group.
-            constexpr int GROUP = [] {
-                int g = BATCHES;
-                while (g * 2 * TM > 20 || BATCHES % g)
-                    --g;
-                return g;
-            }();
-#pragma unroll
-            for (int b0 = 0; b0 < BATCHES; b0 += GROUP) {
-                f32x4 sum[GROUP][2][TM];
-                for (int sp = 0; sp < splits; ++sp) {
-                    const uint32_t base = wave_base(sp) + b0 * TM * 2 * 1024u;
-                    f32x4 x[GROUP][2][TM];
-#pragma unroll
-                    for (int g = 0; g < GROUP; ++g)
-#pragma unroll
-                        for (int mi = 0; mi < TM; ++mi)
-#pragma unroll
-                            for (int sa = 0; sa < 2; ++sa)
-                                x[g][sa][mi] = __builtin_bit_cast(
-                                    f32x4, __builtin_amdgcn_raw_buffer_load_b128(
-                                               prs, lane_off, base + ((g * TM + mi) * 2 + sa) * 1024u, kCoherent));
-#pragma unroll
-                    for (int g = 0; g < GROUP; ++g)
+                    for (int mi = 0; mi < TM; ++mi)
 #pragma unroll
                         for (int sa = 0; sa < 2; ++sa)
+                            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u32x4, piece(b, mi, sa)), prs, lane_off,
+                                                                   own + ((b * TM + mi) * 2 + sa) * 1024u, kCoherent);
+                wait_vmcnt<0>();
+                __syncthreads();
+                if (tid == 0) {
+                    const uint32_t before =
+                        __hip_atomic_fetch_add(p.counters + piece_tile, 1u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                    s_last = before == (uint32_t)(splits - 1);
+                }
+                __syncthreads();
+                if (!s_last)
+                    return;
+                if (tid == 0)
+                    __hip_atomic_store(p.counters + piece_tile, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+                first_gates();
+                // GROUP batches' sums at once: the loads of one split, of up to 20 pieces, are
+                // in flight together, and each split costs their latency for every group.
+                // Fewer beside the accumulators of a 256-row tile, which more would spill.
+                constexpr int GROUP = [] {
+                    int g = BATCHES, most = PIECES < 32 ? 20 : DH ? 4 : 8;
+                    while (g * 2 * TM > most || BATCHES % g)
+                        --g;
+                    return g;
+                }();
+#pragma unroll
+                for (int b0 = 0; b0 < BATCHES; b0 += GROUP) {
+                    f32x4 sum[GROUP][2][TM];
+                    for (int sp = 0; sp < splits; ++sp) {
+                        const uint32_t base = wave_base(sp) + b0 * TM * 2 * 1024u;
+                        f32x4 x[GROUP][2][TM];
+#pragma unroll
+                        for (int g = 0; g < GROUP; ++g)
 #pragma unroll
                             for (int mi = 0; mi < TM; ++mi)
-                                sum[g][sa][mi] = sp == 0 ? x[g][sa][mi] : sum[g][sa][mi] + x[g][sa][mi];
+#pragma unroll
+                                for (int sa = 0; sa < 2; ++sa)
+                                    x[g][sa][mi] = __builtin_bit_cast(
+                                        f32x4, __builtin_amdgcn_raw_buffer_load_b128(
+                                                   prs, lane_off, base + ((g * TM + mi) * 2 + sa) * 1024u, kCoherent));
+#pragma unroll
+                        for (int g = 0; g < GROUP; ++g)
+#pragma unroll
+                            for (int sa = 0; sa < 2; ++sa)
+#pragma unroll
+                                for (int mi = 0; mi < TM; ++mi)
+                                    sum[g][sa][mi] = sp == 0 ? x[g][sa][mi] : sum[g][sa][mi] + x[g][sa][mi];
+                    }
+#pragma unroll
+                    for (int g = 0; g < GROUP; ++g)
+                        emit(b0 + g, sum[g][0], sum[g][1]);
                 }
-#pragma unroll
-                for (int g = 0; g < GROUP; ++g)
-                    emit(b0 + g, sum[g][0], sum[g][1]);
+                return;
             }
-            return;
         }
-    }
-    first_gates();
+        first_gates();
 #pragma unroll
-    for (int b = 0; b < BATCHES; ++b) {
-        f32x4 lo[TM], hi[TM];
+        for (int b = 0; b < BATCHES; ++b) {
+            f32x4 lo[TM], hi[TM];
 #pragma unroll
-        for (int mi = 0; mi < TM; ++mi) {
-            lo[mi] = piece(b, mi, 0);
-            hi[mi] = piece(b, mi, 1);
+            for (int mi = 0; mi < TM; ++mi) {
+                lo[mi] = piece(b, mi, 0);
+                hi[mi] = piece(b, mi, 1);
+            }
+            emit(b, lo, hi);
         }
-        emit(b, lo, hi);
+    };
+    // A tile whose rows end early leaves out the blocks behind them.
+    if constexpr (!WEIGHTS && TN > 1) {
+        const int rows = N - n0;
+        if (rows <= S::WN * 32)
+            return run.template operator()<1>();
+        if constexpr (TN > 2)
+            if (rows <= S::WN * 64)
+                return run.template operator()<2>();
     }
+    run.template operator()<TN>();
 }
 
 } // namespace gmlp
