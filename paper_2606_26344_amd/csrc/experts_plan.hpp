@@ -87,7 +87,7 @@ inline double rows_per_expert(int64_t N, int64_t E) { return (double)N / (double
 inline int grouped_tile_rows(int64_t N, int64_t E)
 {
     const double n = rows_per_expert(N, E);
-    return n <= 24 ? 32 : n <= 48 ? 64 : n <= 160 ? 128 : 256;
+    return n <= 24 ? 32 : n <= 48 ? 64 : n <= 112 ? 128 : 256;
 }
 
 // A product of M columns with `segments` contractions of K each, on tiles of ROWS rows.
@@ -125,14 +125,18 @@ GroupedStep grouped_step(int64_t N, int64_t E, int64_t M, int64_t K, int segment
                              [&](auto rows) { return grouped_step<OP, decltype(rows)::value>(N, E, M, K, segments); });
 }
 
-// Tiles of the weight gradients, by the rows of an expert (measured for one expert, see
-// grad_plan.hpp).
+// Tiles of the weight gradients, by the rows of an expert (those for one expert are
+// measured in grad_plan.hpp).  Three blocks to a CU where a tile has one k-tile or so: its
+// loads and its outputs go on beside those of the others (us for the three steps of the
+// backward pass, with the pair in brackets: 8 experts of 4096 x 14336, 4 rows each 1031
+// [1098]; 64 of 2048 x 1024, 2 rows 269 [273], 64 rows 446 [443]).
+using GradThin = GradShape<2, 2, 2, 2, 2, 32, 3>; // 128 x 128, 4 waves, three blocks on a CU
 inline GradTile grouped_weight_tile(int64_t N, int64_t E, int64_t D, int64_t F)
 {
     const double n = rows_per_expert(N, E);
     if (n <= 256 && 3 * E * cdiv(D, 128) * cdiv(F, 256) <= 2 * kBlockTarget)
         return GRAD_SHORT;
-    return n <= 1536 ? GRAD_PAIR : GRAD_LARGE;
+    return n <= 32 ? GRAD_SMALL : n <= 1536 ? GRAD_PAIR : GRAD_LARGE;
 }
 
 // f(GradShapeTag) of a tile of the weight gradients.
@@ -141,6 +145,7 @@ auto with_grouped_weight_tile(GradTile t, F f)
 {
     switch (t) {
     case GRAD_SHORT: return f(GradShapeTag<GradShort, GRAD_SHORT>{});
+    case GRAD_SMALL: return f(GradShapeTag<GradThin, GRAD_SMALL>{});
     case GRAD_PAIR: return f(GradShapeTag<GradPair, GRAD_PAIR>{});
     default: return f(GradShapeTag<GradLarge, GRAD_LARGE>{});
     }
@@ -196,7 +201,7 @@ inline GroupedLayout grouped_layout(int64_t N, int64_t E, int64_t D, int64_t F)
     // Fewer rows have smaller tiles, with fewer sums; those of any tile up to this
     // call's are provided for.
     size_t partial = 0;
-    for (int64_t n : {N, std::min(N, 160 * E), std::min(N, 48 * E), std::min(N, 24 * E)}) {
+    for (int64_t n : {N, std::min(N, 112 * E), std::min(N, 48 * E), std::min(N, 24 * E)}) {
         const GroupedPlan p = grouped_plan(n, E, D, F);
         partial = std::max({partial, p.gate_up.partial_bytes, p.save.partial_bytes, p.down.partial_bytes, p.dh.partial_bytes,
                             p.dx.partial_bytes});

@@ -79,6 +79,18 @@ int with_choices(int64_t k, F f)
            : k <= 4 ? f(integral_constant<int, 4>{}) : f(integral_constant<int, 8>{});
 }
 
+// Whether sorted rows are more than the L2s of the eight XCDs hold.  us, past the L2
+// against through it: gradients of combine, 268 MB 108 against 116, 67 MB 29 against 33,
+// 34 MB 17.2 against 14.3; combine, 268 MB 63.5 against 65.3.
+bool past_l2(size_t bytes) { return bytes > (size_t)32 << 20; }
+
+// f(bool) as an integral constant.
+template <class F>
+int with_flag(bool b, F f)
+{
+    return b ? f(std::true_type{}) : f(std::false_type{});
+}
+
 int launched(const char *what)
 {
     const int rc = hip_check(hipGetLastError(), what);
@@ -116,15 +128,23 @@ int gmlp_route_sort(const void *ids, void *offsets, void *slots, int64_t T, int6
     p.experts = (int)E;
     while ((1 << p.bits) < E)
         ++p.bits;
-    const int64_t blocks = std::clamp<int64_t>(cdiv(n, 2 * kSortThreads), 1, 128);
-    p.chunk = (int)(std::max<int64_t>(1, cdiv(n, blocks * kSortThreads)) * kSortThreads);
-    const dim3 grid((unsigned)std::max<int64_t>(1, cdiv(n, p.chunk))), block(kSortThreads);
     hipStream_t st = static_cast<hipStream_t>(stream);
-    if (id == 8)
-        hipLaunchKernelGGL(route_sort_kernel<int64_t>, grid, block, 0, st, p);
-    else
-        hipLaunchKernelGGL(route_sort_kernel<int32_t>, grid, block, 0, st, p);
-    return launched("sort launch");
+    const bool one = n <= kSortOneLaunch;
+    // Chunks of 2048 assignments, no less than the experts; more where there would be many.
+    p.chunk = 2 * kSortThreads * (int)std::max<int64_t>(1, n / (2048 * 512));
+    p.blocks = (int)std::max<int64_t>(1, n / p.chunk);
+    return with_flag(id == 8, [&](auto wide) {
+        using Id = std::conditional_t<decltype(wide)::value, int64_t, int32_t>;
+        const dim3 grid((unsigned)p.blocks), block(kSortThreads);
+        if (one) {
+            hipLaunchKernelGGL(route_sort_kernel<Id>, grid, block, 0, st, p);
+            return launched("sort launch");
+        }
+        hipLaunchKernelGGL(route_count_kernel<Id>, grid, block, 0, st, p);
+        hipLaunchKernelGGL(route_scan_kernel, dim3(1), block, 0, st, p);
+        hipLaunchKernelGGL(route_place_kernel<Id>, grid, block, 0, st, p);
+        return launched("sort launch");
+    });
 }
 
 int gmlp_route_dispatch(const void *X, const void *slots, void *xs, int64_t T, int64_t k, int64_t D, void *stream)
@@ -167,11 +187,15 @@ int gmlp_route_combine(const void *ys, const void *slots, const void *weights, v
     const dim3 grid((unsigned)cdiv(T, kRouteThreads >> p.lanes_log)), block(kRouteThreads);
     hipStream_t st = static_cast<hipStream_t>(stream);
     return with_choices(k, [&](auto choices) {
-        constexpr int J = decltype(choices)::value;
-        auto *kernel = !weights ? route_combine_kernel<J, ROUTE_ONES>
-                                : wb == 2 ? route_combine_kernel<J, ROUTE_BF16> : route_combine_kernel<J, ROUTE_FP32>;
-        hipLaunchKernelGGL(kernel, grid, block, 0, st, p);
-        return launched("combine launch");
+        return with_flag(past_l2(2 * n * D), [&](auto once) {
+            constexpr int J = decltype(choices)::value;
+            constexpr bool ONCE = decltype(once)::value;
+            auto *kernel = !weights  ? route_combine_kernel<J, ROUTE_ONES, ONCE>
+                           : wb == 2 ? route_combine_kernel<J, ROUTE_BF16, ONCE>
+                                     : route_combine_kernel<J, ROUTE_FP32, ONCE>;
+            hipLaunchKernelGGL(kernel, grid, block, 0, st, p);
+            return launched("combine launch");
+        });
     });
 }
 
@@ -197,15 +221,22 @@ int gmlp_route_combine_backward(const void *dY, const void *ys, const void *slot
     p.weights = weights;
     p.dweights = dweights;
     hipStream_t st = static_cast<hipStream_t>(stream);
-    // A wave for each token, or the four of a block where tokens are few.
-    const bool four = T <= 2048 && p.chunks > 64;
-    const dim3 grid((unsigned)cdiv(T, four ? 1 : 4)), block(kRouteThreads);
+    // As many waves for a token, up to the four of a block, as its row has chunks for (us,
+    // against one: 4096 tokens, 8 choices, 4096 columns 108 and 129, 2 choices 29 and 34).
+    const int waves = p.chunks > 128 ? 4 : p.chunks > 64 ? 2 : 1;
+    const dim3 grid((unsigned)cdiv(T, 4 / waves)), block(kRouteThreads);
     return with_choices(k, [&](auto choices) {
-        constexpr int J = decltype(choices)::value;
-        auto *kernel = four ? (wb == 2 ? route_combine_backward_kernel<J, 4, true> : route_combine_backward_kernel<J, 4, false>)
-                            : (wb == 2 ? route_combine_backward_kernel<J, 1, true> : route_combine_backward_kernel<J, 1, false>);
-        hipLaunchKernelGGL(kernel, grid, block, 0, st, p);
-        return launched("combine backward launch");
+        return with_flag(wb == 2, [&](auto bf16) {
+            return with_flag(past_l2(2 * n * D), [&](auto once) {
+                constexpr int J = decltype(choices)::value;
+                constexpr bool BF16 = decltype(bf16)::value, ONCE = decltype(once)::value;
+                auto *kernel = waves == 4   ? route_combine_backward_kernel<J, 4, BF16, ONCE>
+                               : waves == 2 ? route_combine_backward_kernel<J, 2, BF16, ONCE>
+                                            : route_combine_backward_kernel<J, 1, BF16, ONCE>;
+                hipLaunchKernelGGL(kernel, grid, block, 0, st, p);
+                return launched("combine backward launch");
+            });
+        });
     });
 }
 

@@ -1,7 +1,7 @@
 // Tokens sorted by expert and back, for gfx950.
 //
-// The sort is a stable counting sort in one launch: its results are whole numbers, so
-// any order of the counting gives the same.  Rows are moved token by token: a token's
+// The sort is a stable counting sort: its results are whole numbers, so any order of the
+// counting gives the same.  Rows are moved token by token: a token's
 // row is read once and written to (or summed from) the k rows of its slots.
 #pragma once
 
@@ -18,8 +18,9 @@ constexpr int kRouteThreads = 256;
 struct SortParams {
     const void *ids;
     int32_t *offsets, *slots;
-    int n;     // assignments
-    int chunk; // of a block, a multiple of kSortThreads
+    int n;      // assignments
+    int chunk;  // of a block, a multiple of kSortThreads
+    int blocks; // the last one takes what is behind the others' chunks too
     int experts;
     int bits; // that tell experts apart
 };
@@ -31,51 +32,28 @@ __device__ __forceinline__ int expert_of(const void *ids, int i, int experts)
     return v >= 0 && v < (Id)experts ? (int)v : -1;
 }
 
-// A block ranks its chunk of the assignments, its waves a sixteenth of that each, and
-// counts all others: those before the chunk and those behind it.  So no block waits for
-// another, at n / 1024 loads per thread in each.
+// Counts the assignments begin + step 0, 1, .. below end, eight loads on their way at
+// once.  counts: `stride` words to an expert.
 template <class Id>
-__global__ __launch_bounds__(kSortThreads) void route_sort_kernel(SortParams p)
+__device__ __forceinline__ void count_experts(const SortParams &p, uint32_t *counts, int stride, int begin, int end, int step)
 {
-    __shared__ uint32_t mine[kSortWaves][kMaxExperts]; // of a wave: counts, then its next slots
-    __shared__ uint32_t before[kMaxExperts], behind[kMaxExperts];
-    __shared__ uint32_t wave_sum[kSortWaves];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, E = p.experts;
-    for (int e = tid; e < E; e += kSortThreads) {
-        before[e] = behind[e] = 0;
-        for (int w = 0; w < kSortWaves; ++w)
-            mine[w][e] = 0;
+    for (int i0 = begin; i0 < end; i0 += 8 * step) {
+        int e[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            e[j] = i0 + j * step < end ? expert_of<Id>(p.ids, i0 + j * step, p.experts) : -1;
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+            if (e[j] >= 0)
+                atomicAdd(&counts[e[j] * stride], 1u);
     }
-    __syncthreads();
-    const int lo = min(p.n, (int)blockIdx.x * p.chunk), hi = min(p.n, lo + p.chunk);
-    for (int i = tid; i < lo; i += kSortThreads) {
-        const int e = expert_of<Id>(p.ids, i, E);
-        if (e >= 0)
-            atomicAdd(&before[e], 1u);
-    }
-    for (int i = hi + tid; i < p.n; i += kSortThreads) {
-        const int e = expert_of<Id>(p.ids, i, E);
-        if (e >= 0)
-            atomicAdd(&behind[e], 1u);
-    }
-    const int part = p.chunk / kSortWaves, first = lo + wave * part, last = min(hi, first + part);
-    for (int i = first + lane; i < last; i += 64) {
-        const int e = expert_of<Id>(p.ids, i, E);
-        if (e >= 0)
-            atomicAdd(&mine[wave][e], 1u);
-    }
-    __syncthreads();
+}
 
-    // Where each expert's rows begin (a thread per expert), and in them this block's
-    // and its waves'.
-    uint32_t total = 0, earlier = 0;
-    if (tid < E) {
-        earlier = before[tid];
-        total = earlier + behind[tid];
-        for (int w = 0; w < kSortWaves; ++w)
-            total += mine[w][tid];
-    }
-    uint32_t sum = total;
+// The sum over the threads before this one.
+__device__ __forceinline__ uint32_t sum_before(uint32_t v, uint32_t (&wave_sum)[kSortWaves])
+{
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    uint32_t sum = v;
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1) {
         const uint32_t up = __shfl_up(sum, d);
@@ -84,9 +62,92 @@ __global__ __launch_bounds__(kSortThreads) void route_sort_kernel(SortParams p)
     if (lane == 63)
         wave_sum[wave] = sum;
     __syncthreads();
-    uint32_t start = sum - total;
+    sum -= v;
     for (int w = 0; w < wave; ++w)
-        start += wave_sum[w];
+        sum += wave_sum[w];
+    return sum;
+}
+
+// A block's assignments: a sixteenth for each wave, whole rounds of 64.
+struct SortRange {
+    int lo, hi, first, last; // of the block, of this wave
+};
+__device__ __forceinline__ SortRange sort_range(const SortParams &p)
+{
+    SortRange r;
+    r.lo = (int)blockIdx.x * p.chunk;
+    r.hi = (int)blockIdx.x + 1 == p.blocks ? p.n : r.lo + p.chunk;
+    const int part = (r.hi - r.lo + kSortThreads - 1) / kSortThreads * 64;
+    r.first = min(r.hi, r.lo + (int)(threadIdx.x >> 6) * part);
+    r.last = min(r.hi, r.first + part);
+    return r;
+}
+
+// The slots of a wave's assignments, `next` its next slot of every expert.  Ranks within
+// 64 of them: the lanes of the same expert, from one vote per bit.
+template <class Id>
+__device__ __forceinline__ void place_slots(const SortParams &p, const SortRange &r, uint32_t *next)
+{
+    const int lane = threadIdx.x & 63;
+    for (int i0 = r.first; i0 < r.last; i0 += 64) {
+        const int i = i0 + lane;
+        const int e = i < r.last ? expert_of<Id>(p.ids, i, p.experts) : -1;
+        uint64_t same = __ballot(e >= 0);
+        for (int b = 0; b < p.bits; ++b) {
+            const uint64_t set = __ballot(e >> b & 1);
+            same &= e >> b & 1 ? set : ~set;
+        }
+        const uint64_t below = same & ((uint64_t(1) << lane) - 1);
+        const uint32_t at = e >= 0 ? next[e] : 0;
+        wave_lds_fence();
+        if (e >= 0 && below == 0) // the first of them moves the slot on for all
+            next[e] = at + (uint32_t)__popcll(same);
+        wave_lds_fence();
+        if (i < r.last)
+            p.slots[i] = e >= 0 ? (int32_t)(at + (uint32_t)__popcll(below)) : -1;
+    }
+}
+
+// Up to kSortOneLaunch assignments: a block ranks its chunk, its waves a sixteenth of
+// that each, and counts all others, those before the chunk and those behind it.  So no
+// block waits for another, but each reads everything, at 50 GB/s for each CU: us, one
+// launch against three, 8 experts and 8192 assignments 5.9 and 15.2, 64 and 32768 10.3 and
+// 10.1, 64 and 65536 15.5 and 10.1, 128 and 524288 95 and 14.5.
+template <class Id>
+__global__ __launch_bounds__(kSortThreads) void route_sort_kernel(SortParams p)
+{
+    __shared__ uint32_t mine[kSortWaves][kMaxExperts]; // of a wave: counts, then its next slots
+    // Four counters each, since lanes that add to one counter take turns (65536 assignments
+    // to one expert 24 us, with one counter 60).
+    __shared__ uint32_t before[kMaxExperts][4], behind[kMaxExperts][4];
+    __shared__ uint32_t wave_sum[kSortWaves];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, E = p.experts;
+    for (int e = tid; e < E; e += kSortThreads) {
+        for (int c = 0; c < 4; ++c)
+            before[e][c] = behind[e][c] = 0;
+        for (int w = 0; w < kSortWaves; ++w)
+            mine[w][e] = 0;
+    }
+    __syncthreads();
+    const SortRange r = sort_range(p);
+    count_experts<Id>(p, &before[0][lane & 3], 4, tid, r.lo, kSortThreads);
+    count_experts<Id>(p, &behind[0][lane & 3], 4, r.hi + tid, p.n, kSortThreads);
+    count_experts<Id>(p, mine[wave], 1, r.first + lane, r.last, 64);
+    __syncthreads();
+
+    // Where each expert's rows begin (a thread per expert), and in them this block's
+    // and its waves'.
+    uint32_t total = 0, earlier = 0;
+    if (tid < E) {
+        for (int c = 0; c < 4; ++c) {
+            earlier += before[tid][c];
+            total += behind[tid][c];
+        }
+        total += earlier;
+        for (int w = 0; w < kSortWaves; ++w)
+            total += mine[w][tid];
+    }
+    const uint32_t start = sum_before(total, wave_sum);
     if (tid < E) {
         if (blockIdx.x == 0) {
             p.offsets[tid] = (int32_t)start;
@@ -101,25 +162,100 @@ __global__ __launch_bounds__(kSortThreads) void route_sort_kernel(SortParams p)
         }
     }
     __syncthreads();
+    place_slots<Id>(p, r, mine[wave]);
+}
 
-    // Ranks within 64 assignments: the lanes of the same expert, from one vote per bit.
-    for (int i0 = first; i0 < last; i0 += 64) {
-        const int i = i0 + lane;
-        const int e = i < last ? expert_of<Id>(p.ids, i, E) : -1;
-        uint64_t same = __ballot(e >= 0);
-        for (int b = 0; b < p.bits; ++b) {
-            const uint64_t set = __ballot(e >> b & 1);
-            same &= e >> b & 1 ? set : ~set;
+// More assignments, in three launches: each block's counts, then where its rows of each
+// expert begin, are kept in its own part of the slots (a chunk is no less than the
+// experts), until the last launch has read them.
+constexpr int kSortOneLaunch = 1 << 15;
+
+template <class Id>
+__global__ __launch_bounds__(kSortThreads) void route_count_kernel(SortParams p)
+{
+    __shared__ uint32_t counts[kMaxExperts][4];
+    const int tid = threadIdx.x;
+    for (int e = tid; e < p.experts; e += kSortThreads)
+        for (int c = 0; c < 4; ++c)
+            counts[e][c] = 0;
+    __syncthreads();
+    const SortRange r = sort_range(p);
+    count_experts<Id>(p, &counts[0][tid & 3], 4, r.lo + tid, r.hi, kSortThreads);
+    __syncthreads();
+    for (int e = tid; e < p.experts; e += kSortThreads)
+        p.slots[r.lo + e] = (int32_t)(counts[e][0] + counts[e][1] + counts[e][2] + counts[e][3]);
+}
+
+// One block: 1 << bits threads walk the experts' counts of a run of blocks.
+__global__ __launch_bounds__(kSortThreads) void route_scan_kernel(SortParams p)
+{
+    __shared__ uint32_t part[kSortThreads]; // counts of an expert in a run of blocks, then their sums
+    __shared__ uint32_t wave_sum[kSortWaves];
+    const int tid = threadIdx.x, E = p.experts;
+    const int e = tid & ((1 << p.bits) - 1), run = tid >> p.bits, runs = min(kSortThreads >> p.bits, p.blocks);
+    const int per = (p.blocks + runs - 1) / runs, first = min(p.blocks, run * per), last = min(p.blocks, first + per);
+    uint32_t sum = 0;
+    if (e < E)
+        for (int b0 = first; b0 < last; b0 += 8)
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                sum += b0 + j < last ? (uint32_t)p.slots[(size_t)(b0 + j) * p.chunk + e] : 0;
+    part[tid] = sum;
+    __syncthreads();
+    uint32_t total = 0;
+    if (tid < E)
+        for (int r = 0; r < runs; ++r) {
+            const uint32_t c = part[(r << p.bits) + tid];
+            part[(r << p.bits) + tid] = total;
+            total += c;
         }
-        const uint64_t below = same & ((uint64_t(1) << lane) - 1);
-        const uint32_t at = e >= 0 ? mine[wave][e] : 0;
-        wave_lds_fence();
-        if (e >= 0 && below == 0) // the first of them moves the slot on for all
-            mine[wave][e] = at + (uint32_t)__popcll(same);
-        wave_lds_fence();
-        if (i < last)
-            p.slots[i] = e >= 0 ? (int32_t)(at + (uint32_t)__popcll(below)) : -1;
+    const uint32_t start = sum_before(total, wave_sum);
+    if (tid < E) {
+        p.offsets[tid] = (int32_t)start;
+        if (tid == E - 1)
+            p.offsets[E] = (int32_t)(start + total);
+        for (int r = 0; r < runs; ++r)
+            part[(r << p.bits) + tid] += start;
     }
+    __syncthreads();
+    uint32_t at = part[tid];
+    if (e < E)
+        for (int b0 = first; b0 < last; b0 += 8) {
+            uint32_t c[8]; // eight blocks' on their way at once
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                c[j] = b0 + j < last ? (uint32_t)p.slots[(size_t)(b0 + j) * p.chunk + e] : 0;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                if (b0 + j < last)
+                    p.slots[(size_t)(b0 + j) * p.chunk + e] = (int32_t)at;
+                at += c[j];
+            }
+        }
+}
+
+template <class Id>
+__global__ __launch_bounds__(kSortThreads) void route_place_kernel(SortParams p)
+{
+    __shared__ uint32_t mine[kSortWaves][kMaxExperts];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6, E = p.experts;
+    for (int e = tid; e < E; e += kSortThreads)
+        for (int w = 0; w < kSortWaves; ++w)
+            mine[w][e] = 0;
+    __syncthreads();
+    const SortRange r = sort_range(p);
+    count_experts<Id>(p, mine[wave], 1, r.first + lane, r.last, 64);
+    __syncthreads();
+    for (int e = tid; e < E; e += kSortThreads) {
+        uint32_t at = (uint32_t)p.slots[r.lo + e];
+        for (int w = 0; w < kSortWaves; ++w) {
+            const uint32_t c = mine[w][e];
+            mine[w][e] = at;
+            at += c;
+        }
+    }
+    __syncthreads(); // every thread has read the starts, which slots take the place of
+    place_slots<Id>(p, r, mine[wave]);
 }
 
 struct RouteParams {
@@ -158,6 +294,14 @@ __device__ __forceinline__ u32x4 *row_chunks(uint16_t *base, int row, int chunks
 {
     return reinterpret_cast<u32x4 *>(base) + (size_t)row * chunks;
 }
+// Sorted rows are read once, and pass the L2 where they are more than it holds.
+template <bool ONCE>
+__device__ __forceinline__ u32x4 load_row(const u32x4 *p)
+{
+    return ONCE ? __builtin_nontemporal_load(p) : *p;
+}
+// They are written for another kernel.
+__device__ __forceinline__ void store_row(u32x4 *p, const u32x4 &v) { __builtin_nontemporal_store(v, p); }
 
 // xs[slot] = x: 1 << lanes_log threads of a block move one token's row.
 __global__ __launch_bounds__(kRouteThreads) void route_dispatch_kernel(RouteParams p)
@@ -172,7 +316,7 @@ __global__ __launch_bounds__(kRouteThreads) void route_dispatch_kernel(RoutePara
         for (int j = 0; j < p.choices; ++j) {
             const int s = slot_of(p, t * p.choices + j);
             if (s >= 0)
-                row_chunks(p.out, s, p.chunks)[c] = v;
+                store_row(row_chunks(p.out, s, p.chunks) + c, v);
         }
     }
 }
@@ -180,7 +324,7 @@ __global__ __launch_bounds__(kRouteThreads) void route_dispatch_kernel(RoutePara
 enum RouteWeights { ROUTE_ONES, ROUTE_FP32, ROUTE_BF16 };
 
 // y = sum_j w_j ys[slot_j], eight columns per thread; up to J rows on their way at once.
-template <int J, int WEIGHTS>
+template <int J, int WEIGHTS, bool ONCE>
 __global__ __launch_bounds__(kRouteThreads) void route_combine_kernel(RouteParams p)
 {
     const int lanes = 1 << p.lanes_log;
@@ -199,7 +343,7 @@ __global__ __launch_bounds__(kRouteThreads) void route_combine_kernel(RouteParam
                 v[j] = u32x4{};
                 w[j] = 0.0f;
                 if (s >= 0) {
-                    v[j] = row_chunks(p.rows, s, p.chunks)[c];
+                    v[j] = load_row<ONCE>(row_chunks(p.rows, s, p.chunks) + c);
                     w[j] = WEIGHTS == ROUTE_ONES ? 1.0f : weight_of<WEIGHTS == ROUTE_BF16>(p, i);
                 }
             }
@@ -219,7 +363,7 @@ __global__ __launch_bounds__(kRouteThreads) void route_combine_kernel(RouteParam
 // dys[slot_j] = w_j dy and dw_j = dy . ys[slot_j]: W waves of a block per token, a lane
 // takes every 64 W-th chunk; the sums of its choices' products stay in registers, J
 // choices at a time.
-template <int J, int W, bool BF16>
+template <int J, int W, bool BF16, bool ONCE>
 __global__ __launch_bounds__(kRouteThreads) void route_combine_backward_kernel(RouteParams p)
 {
     constexpr int TOKENS = kRouteThreads / 64 / W; // of a block
@@ -245,7 +389,7 @@ __global__ __launch_bounds__(kRouteThreads) void route_combine_backward_kernel(R
                 for (int j = 0; j < J; ++j) {
                     v[j] = u32x4{};
                     if (slot[j] >= 0 && p.dweights)
-                        v[j] = row_chunks(p.rows, slot[j], p.chunks)[c];
+                        v[j] = load_row<ONCE>(row_chunks(p.rows, slot[j], p.chunks) + c);
                 }
 #pragma unroll
                 for (int j = 0; j < J; ++j) {
@@ -260,7 +404,7 @@ __global__ __launch_bounds__(kRouteThreads) void route_combine_backward_kernel(R
                         o[q] = pack_bf16x2(w[j] * lo, w[j] * hi);
                     }
                     if (slot[j] >= 0 && p.out)
-                        row_chunks(p.out, slot[j], p.chunks)[c] = o;
+                        store_row(row_chunks(p.out, slot[j], p.chunks) + c, o);
                 }
             }
         if (!p.dweights)

@@ -50,7 +50,8 @@ def random_ids(T, k, E, seed, kind="some", dtype=torch.int32):
 
 @pytest.mark.parametrize("T,k,E", [(1, 1, 1), (1, 2, 8), (1, 64, 1024), (33, 8, 64), (63, 1, 2), (64, 1, 3), (65, 1, 256),
                                    (500, 4, 60), (1024, 2, 8), (1025, 2, 9), (2049, 7, 1000), (4096, 8, 256),
-                                   (30011, 3, 17), (70001, 8, 128)])
+                                   (30011, 3, 17), (32768, 1, 64), (32769, 1, 1024),
+                                   (70001, 8, 128), (70001, 3, 1), (33333, 2, 1000), (1048579, 8, 5)])
 @pytest.mark.parametrize("kind", ["all", "some", "one", "none"])
 def test_sort(T, k, E, kind):
     print("sort", T, k, E, kind, flush=True)
