@@ -30,12 +30,12 @@ struct GroupedShape;
 template <>
 struct GroupedShape<32> {
     using GateUp = GradShape<4, 1, 2, 1, 4, 64, 1>;
-    using Other = GradTall32;
+    using Other = GradShape<4, 1, 1, 1, 3, 64, 1>;
 };
 template <>
 struct GroupedShape<64> {
     using GateUp = GradShape<4, 1, 2, 2, 3, 64, 1>;
-    using Other = GradTall64;
+    using Other = GradShape<4, 1, 1, 2, 3, 64, 1>;
 };
 template <>
 struct GroupedShape<128> {

@@ -133,6 +133,8 @@ struct GradLoader {
     }
 
     // The DMA of the k-tile from k0 on: k past krem and lines past L read as zeros.
+    // STREAM: elements that no other block reads.
+    template <bool STREAM = false>
     __device__ __forceinline__ void issue(const uint16_t *p, int k0, int krem, uint8_t *buf, int wave, int lane) const
     {
         const __amdgpu_buffer_rsrc_t rs = make_rsrc(p + start + (size_t)k0 * k_stride);
@@ -141,7 +143,11 @@ struct GradLoader {
             const int b = which(i);
             const bool in_k = (KC ? first_k(b, wave, lane) : i * RPI + wave * LPR + lane / CPR) < krem;
             const bool in = in_k && (!KC || i * ROW_STEP + line(b, wave, lane) < lines);
-            load16_to_lds(rs, buf + (i * NWAVES + wave) * 1024, in ? voff[b] : kOutOfRange, (uint32_t)i * soff_step);
+            const uint32_t at = in ? voff[b] : kOutOfRange;
+            if constexpr (STREAM)
+                load16_to_lds_stream(rs, buf + (i * NWAVES + wave) * 1024, at, (uint32_t)i * soff_step);
+            else
+                load16_to_lds(rs, buf + (i * NWAVES + wave) * 1024, at, (uint32_t)i * soff_step);
         }
     }
 };
