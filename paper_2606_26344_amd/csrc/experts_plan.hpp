@@ -84,10 +84,27 @@ auto with_grouped_rows(int rows, F f)
 // Rows of an expert where they are spread evenly over as many experts as can have some.
 inline double rows_per_expert(int64_t N, int64_t E) { return (double)N / (double)std::max<int64_t>(1, std::min(N, E)); }
 
-inline int grouped_tile_rows(int64_t N, int64_t E)
+// The most rows that a tile of a call has: where the weights fill the chip with tiles, those
+// that the experts' rows go into once, with room for more than the mean.
+inline int most_tile_rows(int64_t N, int64_t E)
 {
     const double n = rows_per_expert(N, E);
-    return n <= 24 ? 32 : n <= 48 ? 64 : n <= 112 ? 128 : 256;
+    return n <= 20 ? 32 : n <= 40 ? 64 : n <= 104 ? 128 : 256;
+}
+
+// Rows of a tile of a product with M columns: fewer, down to 32, while half the CUs have no
+// tile.  Measured with each (forward pass, us, for 32, 64, 128 and 256 rows; rows of experts
+// spread by 3 : 1):
+//   8 of 4096 x 14336   16 rows each 455 455 467 530   32  594 469 477 540   64 1042 729 509 561
+//                       96          1324 857 579 606  128 1787 1142 700 640
+//   32 of 2048 x 1024   32            92  74  76  82   64  147 106  83  84  128 232 155 130 101
+//   8 of 1024 x 512     64            23  27  30  39  300   47  34  34  51  600  72  58  45  47
+inline int grouped_tile_rows(int64_t N, int64_t E, int64_t M)
+{
+    int rows = most_tile_rows(N, E);
+    while (rows > 32 && (N / rows + std::min(E, N) / 2) * cdiv(M, 128) < kBlockTarget / 2)
+        rows /= 2;
+    return rows;
 }
 
 // A product of M columns with `segments` contractions of K each, on tiles of ROWS rows.
@@ -121,22 +138,22 @@ GroupedStep grouped_step(int64_t N, int64_t E, int64_t M, int64_t K, int segment
 template <GroupedOp OP>
 GroupedStep grouped_step(int64_t N, int64_t E, int64_t M, int64_t K, int segments = 1)
 {
-    return with_grouped_rows(grouped_tile_rows(N, E),
+    return with_grouped_rows(grouped_tile_rows(N, E, M),
                              [&](auto rows) { return grouped_step<OP, decltype(rows)::value>(N, E, M, K, segments); });
 }
 
-// Tiles of the weight gradients, by the rows of an expert (those for one expert are
-// measured in grad_plan.hpp).  Three blocks to a CU where a tile has one k-tile or so: its
-// loads and its outputs go on beside those of the others (us for the three steps of the
-// backward pass, with the pair in brackets: 8 experts of 4096 x 14336, 4 rows each 1031
-// [1098]; 64 of 2048 x 1024, 2 rows 269 [273], 64 rows 446 [443]).
-using GradThin = GradShape<2, 2, 2, 2, 2, 32, 3>; // 128 x 128, 4 waves, three blocks on a CU
+// Tiles of the weight gradients, by the rows of an expert.  Up to 96, and for small
+// weights, four blocks of small tiles to a CU, whose loads and outputs go on beside each
+// other's.  us, the three steps of the backward pass, small tiles and the pair: 8 experts of
+// 4096 x 14336, 4 rows each 958 and 1019, 40 1051 and 1132, 90 1231 and 1283, 128 1465 and
+// 1478; 64 of 2048 x 1024, 2 rows 220 and 245, 50 338 and 357, 128 552 and 543; 8 of 1024 x
+// 512, 128 rows 84 and 86.  From 1536 rows on as in grad_plan.hpp.
+using GradThin = GradShape<2, 2, 2, 2, 2, 32, 4>; // 128 x 128, 4 waves, four blocks on a CU
 inline GradTile grouped_weight_tile(int64_t N, int64_t E, int64_t D, int64_t F)
 {
     const double n = rows_per_expert(N, E);
-    if (n <= 256 && 3 * E * cdiv(D, 128) * cdiv(F, 256) <= 2 * kBlockTarget)
-        return GRAD_SHORT;
-    return n <= 32 ? GRAD_SMALL : n <= 1536 ? GRAD_PAIR : GRAD_LARGE;
+    const bool few = 3 * E * cdiv(D, 128) * cdiv(F, 256) <= 2 * kBlockTarget;
+    return n <= (few ? 256 : 96) ? GRAD_SMALL : n <= 1536 ? GRAD_PAIR : GRAD_LARGE;
 }
 
 // f(GradShapeTag) of a tile of the weight gradients.
@@ -144,7 +161,6 @@ template <class F>
 auto with_grouped_weight_tile(GradTile t, F f)
 {
     switch (t) {
-    case GRAD_SHORT: return f(GradShapeTag<GradShort, GRAD_SHORT>{});
     case GRAD_SMALL: return f(GradShapeTag<GradThin, GRAD_SMALL>{});
     case GRAD_PAIR: return f(GradShapeTag<GradPair, GRAD_PAIR>{});
     default: return f(GradShapeTag<GradLarge, GRAD_LARGE>{});
@@ -198,14 +214,16 @@ inline GroupedLayout grouped_layout(int64_t N, int64_t E, int64_t D, int64_t F)
     l.dg_off = l.h_off + h;
     l.du_off = l.dg_off + h;
     l.partial_off = l.du_off + h;
-    // Fewer rows have smaller tiles, with fewer sums; those of any tile up to this
-    // call's are provided for.
+    // Fewer rows may have smaller tiles: those of any tile up to this call's most.
     size_t partial = 0;
-    for (int64_t n : {N, std::min(N, 112 * E), std::min(N, 48 * E), std::min(N, 24 * E)}) {
-        const GroupedPlan p = grouped_plan(n, E, D, F);
-        partial = std::max({partial, p.gate_up.partial_bytes, p.save.partial_bytes, p.down.partial_bytes, p.dh.partial_bytes,
-                            p.dx.partial_bytes});
-    }
+    for (int rows = 32; rows <= most_tile_rows(std::max<int64_t>(N, 1), E); rows *= 2)
+        with_grouped_rows(rows, [&](auto r) {
+            constexpr int ROWS = decltype(r)::value;
+            for (const GroupedStep &s : {grouped_step<GROUPED_GATE_UP, ROWS>(1, E, F, D, 1), grouped_step<GROUPED_DOWN, ROWS>(1, E, D, F, 1),
+                                         grouped_step<GROUPED_DH, ROWS>(1, E, F, D, 1), grouped_step<GROUPED_DX, ROWS>(1, E, D, F, 2)})
+                partial = std::max(partial, s.partial_bytes);
+            return 0;
+        });
     l.total = l.partial_off + align_up(partial);
     l.counters = 2 * kBlockTarget; // of the tiles that are split: at most as many as run at once
     return l;

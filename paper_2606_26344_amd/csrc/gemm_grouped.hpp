@@ -114,6 +114,7 @@ __global__ __launch_bounds__(S::NTHREADS, S::BLOCKS) void gemm_grouped_kernel(Gr
     constexpr int SEGS = OP == GROUPED_DX ? 2 : 1;
     constexpr int TM = S::TM, TN = S::TN, STAGES = S::STAGES, BK = S::BK;
     constexpr int TMW = TM / NW, BMW = S::BM / NW; // of one weight
+    constexpr bool SIMPLE = S::BLOCKS > 2; // the weight gradients of few rows
     constexpr int OUT_POLICY = STREAM_OUT ? kNonTemporal : 0;
     __shared__ __attribute__((aligned(1024))) uint8_t lds0[S::STAGE_BYTES];
     __shared__ __attribute__((aligned(1024))) uint8_t lds1[S::STAGE_BYTES];
@@ -250,75 +251,108 @@ __global__ __launch_bounds__(S::NTHREADS, S::BLOCKS) void gemm_grouped_kernel(Gr
                 for (int j = 0; j < 4; ++j)
                     acc[mi][ni].set_piece(j, f32x4{});
 
-        // The MFMAs of one k32 step, one group per 16-row B fragment, with the next
-        // step's fragment reads among them (as gemm_grad.hpp).
-        struct FragA {
-            bf16x8 a[TM * 2];
-        };
-        FragA fa0, fa1;
-        bf16x8 fb[TX * 2];
-        auto mma_roll = [&](const FragA &fa, FragA &fa_next, const uint8_t *nbuf, int nkk) __attribute__((always_inline)) {
-            constexpr int GROUPS = TX * 2, AFRAGS = TM * 2, APG = (AFRAGS + GROUPS - 1) / GROUPS;
-            [&]<int... G>(std::integer_sequence<int, G...>) __attribute__((always_inline)) {
-                (
-                    [&] {
+        if constexpr (SIMPLE) {
+            // One stage is computed while the other is on its way, fragments as they are
+            // needed: few registers, so that four blocks are on a CU.
+            static_assert(!SIMPLE || (BK == 32 && STAGES == 2), "two stages of one k32 step");
+            auto step = [&](auto s) __attribute__((always_inline)) {
+                wait_vmcnt<LOADS>();
+                barrier_only();
+                const uint8_t *buf = stage_ptr(s);
+                bf16x8 fa[TM * 2];
 #pragma unroll
-                        for (int a = 0; a < AFRAGS; ++a)
-                            acc[a / 2][G / 2].v[a % 2 + 2 * (G % 2)] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
-                                fa.a[a], fb[G], acc[a / 2][G / 2].v[a % 2 + 2 * (G % 2)], 0, 0, 0);
+                for (int q = 0; q < TM * 2; ++q)
+                    fa[q] = read_a(buf, 0, q);
 #pragma unroll
-                        for (int q = G * APG; q < (G + 1) * APG && q < AFRAGS; ++q)
-                            fa_next.a[q] = read_a(nbuf, nkk, q);
-                        fb[G] = qb.read(nbuf + S::A_BYTES, nkk, G);
-                        __builtin_amdgcn_sched_barrier(0);
-                    }(),
-                    ...);
-            }(std::make_integer_sequence<int, GROUPS>{});
-        };
-        auto wait_tile = [&]() __attribute__((always_inline)) {
-            wait_vmcnt<(STAGES - 2) * LOADS>();
-            wait_lgkm0();
-            barrier_only();
-        };
+                for (int g = 0; g < TX * 2; ++g) {
+                    const bf16x8 fb = qb.read(buf + S::A_BYTES, 0, g);
+#pragma unroll
+                    for (int a = 0; a < TM * 2; ++a)
+                        acc[a / 2][g / 2].v[a % 2 + 2 * (g % 2)] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                            fa[a], fb, acc[a / 2][g / 2].v[a % 2 + 2 * (g % 2)], 0, 0, 0);
+                }
+                wait_lgkm0();
+                barrier_only();
+                issue(stage_ptr(s));
+            };
+            issue(lds0);
+            issue(lds1);
+            for (int i = 0; i < nk; i += 2) {
+                step(std::integral_constant<int, 0>{});
+                if (i + 1 < nk)
+                    step(std::integral_constant<int, 1>{});
+            }
+        } else {
+            // The MFMAs of one k32 step, one group per 16-row B fragment, with the next
+            // step's fragment reads among them (as gemm_grad.hpp).
+            struct FragA {
+                bf16x8 a[TM * 2];
+            };
+            FragA fa0, fa1;
+            bf16x8 fb[TX * 2];
+            auto mma_roll = [&](const FragA &fa, FragA &fa_next, const uint8_t *nbuf, int nkk) __attribute__((always_inline)) {
+                constexpr int GROUPS = TX * 2, AFRAGS = TM * 2, APG = (AFRAGS + GROUPS - 1) / GROUPS;
+                [&]<int... G>(std::integer_sequence<int, G...>) __attribute__((always_inline)) {
+                    (
+                        [&] {
+#pragma unroll
+                            for (int a = 0; a < AFRAGS; ++a)
+                                acc[a / 2][G / 2].v[a % 2 + 2 * (G % 2)] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                                    fa.a[a], fb[G], acc[a / 2][G / 2].v[a % 2 + 2 * (G % 2)], 0, 0, 0);
+#pragma unroll
+                            for (int q = G * APG; q < (G + 1) * APG && q < AFRAGS; ++q)
+                                fa_next.a[q] = read_a(nbuf, nkk, q);
+                            fb[G] = qb.read(nbuf + S::A_BYTES, nkk, G);
+                            __builtin_amdgcn_sched_barrier(0);
+                        }(),
+                        ...);
+                }(std::make_integer_sequence<int, GROUPS>{});
+            };
+            auto wait_tile = [&]() __attribute__((always_inline)) {
+                wait_vmcnt<(STAGES - 2) * LOADS>();
+                wait_lgkm0();
+                barrier_only();
+            };
 
-        [&]<int... I>(std::integer_sequence<int, I...>) __attribute__((always_inline)) {
-            (issue(stage_ptr(std::integral_constant<int, I>{})), ...);
-        }(std::make_integer_sequence<int, STAGES - 1>{});
-        wait_tile();
-        issue(stage_ptr(std::integral_constant<int, STAGES - 1>{}));
-#pragma unroll
-        for (int q = 0; q < TM * 2; ++q)
-            fa0.a[q] = read_a(lds0, 0, q);
-#pragma unroll
-        for (int q = 0; q < TX * 2; ++q)
-            fb[q] = qb.read(lds0 + S::A_BYTES, 0, q);
-        // The k-tile in stage I % STAGES.  At its last k32 step, whose fragments have
-        // been read, a barrier frees the stage for the DMA of the k-tile STAGES ahead
-        // and the next k-tile's first fragments are read.
-        auto step = [&](auto index) __attribute__((always_inline)) {
-            constexpr int I = decltype(index)::value;
-            uint8_t *buf = stage_ptr(std::integral_constant<int, I % STAGES>{});
-            uint8_t *next = stage_ptr(std::integral_constant<int, (I + 1) % STAGES>{});
-            if constexpr (BK == 64)
-                mma_roll(fa0, fa1, buf, 1);
-            wait_tile();
-            issue(buf);
-            if constexpr (BK == 64 || I % 2 == 1)
-                mma_roll(fa1, fa0, next, 0);
-            else
-                mma_roll(fa0, fa1, next, 0);
-        };
-        // A round of steps brings stages and fragment buffers back to the first.
-        constexpr int ROUND = BK == 64 || STAGES % 2 == 0 ? STAGES : 2 * STAGES;
-        int i = 0;
-        for (; i + ROUND <= nk; i += ROUND) {
             [&]<int... I>(std::integer_sequence<int, I...>) __attribute__((always_inline)) {
-                (step(std::integral_constant<int, I>{}), ...);
-            }(std::make_integer_sequence<int, ROUND>{});
+                (issue(stage_ptr(std::integral_constant<int, I>{})), ...);
+            }(std::make_integer_sequence<int, STAGES - 1>{});
+            wait_tile();
+            issue(stage_ptr(std::integral_constant<int, STAGES - 1>{}));
+#pragma unroll
+            for (int q = 0; q < TM * 2; ++q)
+                fa0.a[q] = read_a(lds0, 0, q);
+#pragma unroll
+            for (int q = 0; q < TX * 2; ++q)
+                fb[q] = qb.read(lds0 + S::A_BYTES, 0, q);
+            // The k-tile in stage I % STAGES.  At its last k32 step, whose fragments have
+            // been read, a barrier frees the stage for the DMA of the k-tile STAGES ahead
+            // and the next k-tile's first fragments are read.
+            auto step = [&](auto index) __attribute__((always_inline)) {
+                constexpr int I = decltype(index)::value;
+                uint8_t *buf = stage_ptr(std::integral_constant<int, I % STAGES>{});
+                uint8_t *next = stage_ptr(std::integral_constant<int, (I + 1) % STAGES>{});
+                if constexpr (BK == 64)
+                    mma_roll(fa0, fa1, buf, 1);
+                wait_tile();
+                issue(buf);
+                if constexpr (BK == 64 || I % 2 == 1)
+                    mma_roll(fa1, fa0, next, 0);
+                else
+                    mma_roll(fa0, fa1, next, 0);
+            };
+            // A round of steps brings stages and fragment buffers back to the first.
+            constexpr int ROUND = BK == 64 || STAGES % 2 == 0 ? STAGES : 2 * STAGES;
+            int i = 0;
+            for (; i + ROUND <= nk; i += ROUND) {
+                [&]<int... I>(std::integer_sequence<int, I...>) __attribute__((always_inline)) {
+                    (step(std::integral_constant<int, I>{}), ...);
+                }(std::make_integer_sequence<int, ROUND>{});
+            }
+            [&]<int... I>(std::integer_sequence<int, I...>) __attribute__((always_inline)) {
+                ((i + I < nk ? step(std::integral_constant<int, I>{}) : void()), ...);
+            }(std::make_integer_sequence<int, ROUND - 1>{});
         }
-        [&]<int... I>(std::integer_sequence<int, I...>) __attribute__((always_inline)) {
-            ((i + I < nk ? step(std::integral_constant<int, I>{}) : void()), ...);
-        }(std::make_integer_sequence<int, ROUND - 1>{});
         wait_vmcnt<0>(); // loads past the end, before LDS is given to another block
         asm volatile("" : "+v"(lane)); // the outputs' addresses are made here, not before the loop
 
