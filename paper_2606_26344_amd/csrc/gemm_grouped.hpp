@@ -10,7 +10,7 @@
 // the forward pass and k-contiguous in the backward pass.
 //
 // Which rows are whose is known on the device only.  A block's waves read the offsets
-// (64 experts at once, one per lane), add up the tiles of rows that the experts before
+// (256 experts at once, four per lane), add up the tiles of rows that the experts before
 // have, and find the expert and the rows of the block's tile; blocks past the last tile
 // end.  All blocks come to the same counts, and so does the split of k where the tiles
 // do not fill the chip: the last, partial round of tiles is given to as many blocks as
@@ -51,15 +51,39 @@ __device__ __forceinline__ void expert_rows(const GroupedParams &p, int e, int &
     count = min(max(p.offsets[e + 1], first), p.rows) - first;
 }
 
-// Tiles of ROWS rows of all experts.
+// The rows of 256 experts from e0 on, four per lane (none past the last expert): one
+// latency for all.
+struct Experts {
+    int first[4], count[4];
+    __device__ __forceinline__ void load(const GroupedParams &p, int e0, int lane)
+    {
+        int lo[4], hi[4];
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            const int e = min(e0 + 64 * g + lane, p.experts - 1);
+            lo[g] = p.offsets[e];
+            hi[g] = p.offsets[e + 1];
+        }
+#pragma unroll
+        for (int g = 0; g < 4; ++g) {
+            first[g] = min(max(lo[g], 0), p.rows);
+            count[g] = e0 + 64 * g + lane < p.experts ? min(max(hi[g], first[g]), p.rows) - first[g] : 0;
+        }
+    }
+};
+
+// Tiles of ROWS rows of all experts; `head`: the first 256.
 template <int ROWS>
-__device__ __forceinline__ int count_row_tiles(const GroupedParams &p, int lane)
+__device__ __forceinline__ int count_row_tiles(const GroupedParams &p, const Experts &head, int lane)
 {
     int tiles = 0;
-    for (int e = lane; e < p.experts; e += 64) {
-        int first, count;
-        expert_rows(p, e, first, count);
-        tiles += (count + ROWS - 1) / ROWS;
+    Experts x = head;
+    for (int e0 = 0; e0 < p.experts; e0 += 256) {
+        if (e0 > 0)
+            x.load(p, e0, lane);
+#pragma unroll
+        for (int g = 0; g < 4; ++g)
+            tiles += (x.count[g] + ROWS - 1) / ROWS;
     }
 #pragma unroll
     for (int d = 1; d < 64; d <<= 1)
@@ -74,30 +98,33 @@ struct RowTile {
 
 // The expert that has row tile r of all (r < count_row_tiles).
 template <int ROWS>
-__device__ __forceinline__ RowTile find_row_tile(const GroupedParams &p, int r, int lane)
+__device__ __forceinline__ RowTile find_row_tile(const GroupedParams &p, const Experts &head, int r, int lane)
 {
     RowTile t{0, 0, 0, 0};
-    for (int e0 = 0; e0 < p.experts; e0 += 64) {
-        int first = 0, count = 0;
-        if (e0 + lane < p.experts)
-            expert_rows(p, e0 + lane, first, count);
-        const int tiles = (count + ROWS - 1) / ROWS;
-        int sum = tiles;
+    Experts x = head;
+    for (int e0 = 0; e0 < p.experts; e0 += 256) {
+        if (e0 > 0)
+            x.load(p, e0, lane);
 #pragma unroll
-        for (int d = 1; d < 64; d <<= 1) {
-            const int up = __shfl_up(sum, d);
-            sum += lane >= d ? up : 0;
+        for (int g = 0; g < 4; ++g) {
+            const int tiles = (x.count[g] + ROWS - 1) / ROWS;
+            int sum = tiles;
+#pragma unroll
+            for (int d = 1; d < 64; d <<= 1) {
+                const int up = __shfl_up(sum, d);
+                sum += lane >= d ? up : 0;
+            }
+            const uint64_t reached = __ballot(t.before + sum > r);
+            if (reached) {
+                const int l = __builtin_ctzll(reached);
+                t.expert = e0 + 64 * g + l;
+                t.first = __builtin_amdgcn_readlane(x.first[g], l);
+                t.count = __builtin_amdgcn_readlane(x.count[g], l);
+                t.before += __builtin_amdgcn_readlane(sum - tiles, l);
+                return t;
+            }
+            t.before += __builtin_amdgcn_readlane(sum, 63);
         }
-        const uint64_t reached = __ballot(t.before + sum > r);
-        if (reached) {
-            const int l = __builtin_ctzll(reached);
-            t.expert = e0 + l;
-            t.first = __builtin_amdgcn_readlane(first, l);
-            t.count = __builtin_amdgcn_readlane(count, l);
-            t.before += __builtin_amdgcn_readlane(sum - tiles, l);
-            return t;
-        }
-        t.before += __builtin_amdgcn_readlane(sum, 63);
     }
     return t;
 }
@@ -164,7 +191,9 @@ __global__ __launch_bounds__(S::NTHREADS, S::BLOCKS) void gemm_grouped_kernel(Gr
             return;
         kt_end = (K + BK - 1) / BK;
     } else {
-        const int row_tiles = count_row_tiles<S::BN>(p, lane);
+        Experts head;
+        head.load(p, 0, lane);
+        const int row_tiles = count_row_tiles<S::BN>(p, head, lane);
         const int tiles = row_tiles * p.columns;
         const int in_rounds = tiles / p.slots * p.slots;
         rest = tiles - in_rounds;
@@ -181,7 +210,7 @@ __global__ __launch_bounds__(S::NTHREADS, S::BLOCKS) void gemm_grouped_kernel(Gr
         split = whole ? 0 : id / rest;
         piece_tile = whole ? 0 : id - split * rest;
         const int tile = whole ? id : in_rounds + piece_tile;
-        const RowTile t = find_row_tile<S::BN>(p, tile / p.columns, lane);
+        const RowTile t = find_row_tile<S::BN>(p, head, tile / p.columns, lane);
         expert = t.expert;
         first = t.first;
         count = t.count;
