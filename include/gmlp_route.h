@@ -29,7 +29,7 @@
  * the gradient of combine would write its row twice).
  *
  * Layout: dense and row-major on the current HIP device: rows 16-byte aligned, D a
- * multiple of 8, the limits of gmlp.h on T k, D and the size of a tensor,
+ * multiple of 8, T k below 2^24, the limits of gmlp.h on D and the size of a tensor,
  * k <= GMLP_ROUTE_MAX_CHOICES, E <= GMLP_MAX_EXPERTS; ids, offsets, slots and weights
  * aligned to their elements.  T == 0 launches nothing but the sort, whose offsets are
  * zeros then.  Ownership, streams and errors are as in gmlp.h; the calls allocate

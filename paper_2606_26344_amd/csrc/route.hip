@@ -19,8 +19,9 @@ int check_choices(int64_t T, int64_t k)
 {
     if (T < 0 || k <= 0)
         return fail(GMLP_ERR_INVALID_ARG, "invalid shape T=%lld k=%lld (need T >= 0, k > 0)", (long long)T, (long long)k);
-    if (k > GMLP_ROUTE_MAX_CHOICES || T > kMaxTokens || T * k > kMaxTokens)
-        return fail(GMLP_ERR_UNSUPPORTED, "T=%lld k=%lld exceeds the supported range (k <= %d, T k <= %lld)", (long long)T,
+    // A block of 256 threads for every token stays below the 2^32 threads of a launch.
+    if (k > GMLP_ROUTE_MAX_CHOICES || T >= kMaxTokens || T * k >= kMaxTokens)
+        return fail(GMLP_ERR_UNSUPPORTED, "T=%lld k=%lld exceeds the supported range (k <= %d, T k < %lld)", (long long)T,
                     (long long)k, GMLP_ROUTE_MAX_CHOICES, (long long)kMaxTokens);
     return GMLP_OK;
 }

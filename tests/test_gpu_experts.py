@@ -231,6 +231,46 @@ def test_rows_and_weights_past_32_bits():
         assert (a[-n:] != 0).any() and (a[-n - 5:-n] == 0).all()
 
 
+@pytest.mark.parametrize("counts,D,F", [([3, 0, 40], 8, 1 << 20), ([300, 5], 8, 1 << 20), ([3, 40], 1 << 20, 8), ([270], 1 << 20, 8)])
+def test_widest(counts, D, F):
+    """The widest D and F.  The sums of 2^20 products are formed 32 at a time: 2^15 roundings
+    of 2^-24 S, where 2^-12 S stands for those of the other tests."""
+    N, E = sum(counts), len(counts)
+    t = inputs(N, E, D, F, 4)
+    offsets = offsets_of(counts)
+    w = (t["wg"], t["wu"], t["wd"])
+    y, g, u = experts.train_forward(t["xs"], offsets, *w)
+    dxs, dwg, _, dwd = experts.backward(t["dys"], t["xs"], offsets, *w, g, u, want=("dxs", "dwg", "dwd"))
+    sums = 2.0 ** -9
+
+    def close(got, ref, terms, rounded=True):
+        assert ((got.double() - ref).abs() <= HALF_STEP * ref.abs() + ((1.02 * 2.0 ** -8 if rounded else 0.0) + sums) * terms + 1e-30).all()
+
+    for e, n in enumerate(counts):
+        if n == 0:
+            assert (dwg[e] == 0).all() and (dwd[e] == 0).all()
+            continue
+        lo = sum(counts[:e])
+        rows = slice(lo + max(0, n - 4), lo + n)  # the last of the expert's; the weights' gradients sum all
+        x, dy, wg, wu, wd = (v.double() for v in (t["xs"][rows], t["dys"][rows], t["wg"][e], t["wu"][e], t["wd"][e]))
+        close(g[rows], x @ wg, x.abs() @ wg.abs(), rounded=False)
+        gd, ud = g[rows].double(), u[rows].double()
+        a, da = act(gd, "silu", 1.0)
+        # g and u were rounded on their way to here, not to y: 2^-8 (1.1 |g| + |act(g)|) |u|
+        # beside the 2^-8 |h| of the rounding of h.
+        h = a * ud
+        close(y[rows], h @ wd, 3.0 * (a.abs() + gd.abs()) * ud.abs() @ wd.abs())
+        dh, dh_terms = dy @ wd.T.contiguous(), dy.abs() @ wd.abs().T.contiguous()
+        dg, du = dh * ud * da, dh * a
+        spread = 1.0 if F > D else 2.0  # of dh, a sum of D products
+        close(dxs[rows], dg @ wg.T + du @ wu.T,
+              (dg.abs() + spread * (dh_terms * ud * da).abs()) @ wg.abs().T + (du.abs() + spread * (dh_terms * a).abs()) @ wu.abs().T)
+        some = slice(lo, lo + n)
+        gd, ud = g[some].double(), u[some].double()
+        h = act(gd, "silu", 1.0)[0] * ud
+        close(dwd[e], h.T @ t["dys"][some].double(), h.abs().T @ t["dys"][some].double().abs())
+
+
 def test_gradients_against_differences():
     """Central differences of <dys, ys> in fp64 around the gradients of the kernels: the
     directional derivatives agree to the roundings of the gradients."""

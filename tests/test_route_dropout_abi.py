@@ -38,7 +38,7 @@ def drop_backward(dout=A, dX=A + 20 * MB, T=16, D=256, p=0.1, seed=1, offset=0, 
 
 def test_sort_refusals():
     assert sort(T=-1) == 1 and sort(k=0) == 1 and sort(E=0) == 1 and sort(E=-3) == 1
-    assert sort(E=1025) == 2 and sort(k=65) == 2 and sort(T=1 << 24, k=2) == 2 and sort(T=1 << 62, k=2) == 2
+    assert sort(E=1025) == 2 and sort(k=65) == 2 and sort(T=1 << 24, k=1) == 2 and sort(T=1 << 23, k=2) == 2 and sort(T=1 << 62, k=2) == 2
     assert sort(flags=4) == 1 and sort(flags=1) == 1
     for name in ("ids", "offsets", "slots"):
         assert sort(**{name: None}) == 1 and name in gmlp.last_error()
@@ -50,7 +50,7 @@ def test_sort_refusals():
 @pytest.mark.parametrize("f", [dispatch, combine, combine_backward])
 def test_row_refusals(f):
     assert f(T=-1) == 1 and f(k=0) == 1 and f(D=0) == 1 and f(D=260) == 2 and f(k=65) == 2
-    assert f(D=(1 << 22) + 8) == 2 and f(T=(1 << 24) + 1, k=1) == 2 and f(T=1 << 22, k=4, D=1 << 15) == 2
+    assert f(D=(1 << 22) + 8) == 2 and f(T=1 << 24, k=1) == 2 and f(T=1 << 22, k=4, D=1 << 15) == 2
     if f is not dispatch:
         assert f(flags=2) == 1
     rows = {dispatch: ("X", "xs"), combine: ("ys", "Y"), combine_backward: ("dY", "ys")}[f]
