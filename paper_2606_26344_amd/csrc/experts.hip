@@ -54,8 +54,10 @@ uint16_t *bf16(void *p) { return static_cast<uint16_t *>(p); }
 
 // A product with a weight, of M columns and segments of K.
 template <GroupedOp OP>
-int launch_rows(const GroupedStep &s, GroupedParams p, int64_t M, int64_t K, const char *what, hipStream_t st)
+int launch_rows(const GroupedStep &s, const GroupedLayout &l, GroupedParams p, int64_t M, int64_t K, const char *what, hipStream_t st)
 {
+    if (s.partial_bytes > l.total - l.partial_off || s.slots > l.counters)
+        return fail(GMLP_ERR_INVALID_ARG, "internal: %zu bytes of partial sums for a workspace without", s.partial_bytes);
     p.M = (int)M;
     p.K = (int)K;
     p.kt_seg = s.kt_seg;
@@ -180,14 +182,14 @@ int gmlp_experts_forward(const void *X, const void *offsets, const void *Wg, con
     p.out[0] = reinterpret_cast<uint16_t *>(ws + l.h_off);
     p.out[1] = bf16(G);
     p.out[2] = bf16(U);
-    rc = G ? launch_rows<GROUPED_SAVE>(first, p, F, D, "gate/up launch", st) : launch_rows<GROUPED_GATE_UP>(first, p, F, D, "gate/up launch", st);
+    rc = G ? launch_rows<GROUPED_SAVE>(first, l, p, F, D, "gate/up launch", st) : launch_rows<GROUPED_GATE_UP>(first, l, p, F, D, "gate/up launch", st);
     if (rc)
         return rc;
     p = base;
     p.a[0] = bf16(Wd);
     p.b[0] = reinterpret_cast<const uint16_t *>(ws + l.h_off);
     p.out[0] = bf16(Y);
-    rc = launch_rows<GROUPED_DOWN>(plan.down, p, D, F, "down launch", st);
+    rc = launch_rows<GROUPED_DOWN>(plan.down, l, p, D, F, "down launch", st);
     return rc ? rc : ok();
 }
 
@@ -237,7 +239,7 @@ int gmlp_experts_backward(const void *dY, const void *X, const void *offsets, co
         p.dg = dG;
         p.du = dU;
         p.h = H;
-        if ((rc = launch_rows<GROUPED_DH>(plan.dh, p, F, D, "dH launch", st)))
+        if ((rc = launch_rows<GROUPED_DH>(plan.dh, l, p, F, D, "dH launch", st)))
             return rc;
     }
     if (rows && dX) {
@@ -247,7 +249,7 @@ int gmlp_experts_backward(const void *dY, const void *X, const void *offsets, co
         p.b[0] = dG;
         p.b[1] = dU;
         p.out[0] = bf16(dX);
-        if ((rc = launch_rows<GROUPED_DX>(plan.dx, p, D, F, "dX launch", st)))
+        if ((rc = launch_rows<GROUPED_DX>(plan.dx, l, p, D, F, "dX launch", st)))
             return rc;
     }
     if (problems) {

@@ -89,22 +89,57 @@ inline double rows_per_expert(int64_t N, int64_t E) { return (double)N / (double
 inline int most_tile_rows(int64_t N, int64_t E)
 {
     const double n = rows_per_expert(N, E);
-    return n <= 20 ? 32 : n <= 40 ? 64 : n <= 104 ? 128 : 256;
+    return n <= 20 ? 32 : n <= 40 ? 64 : n <= 112 ? 128 : 256;
 }
 
-// Rows of a tile of a product with M columns: fewer, down to 32, while half the CUs have no
-// tile.  Measured with each (forward pass, us, for 32, 64, 128 and 256 rows; rows of experts
+// Rows of a tile of a product with M columns and K contracted elements: fewer, down to 32,
+// while half the CUs have no tile.  Weights that the last-level cache holds may be read
+// by two tiles of 128 rows for one of 256: there a quarter of the CUs without will do.
+// Measured with each (forward pass, us, for 32, 64, 128 and 256 rows; rows of experts
 // spread by 3 : 1):
 //   8 of 4096 x 14336   16 rows each 455 455 467 530   32  594 469 477 540   64 1042 729 509 561
 //                       96          1324 857 579 606  128 1787 1142 700 640
 //   32 of 2048 x 1024   32            92  74  76  82   64  147 106  83  84  128 232 155 130 101
 //   8 of 1024 x 512     64            23  27  30  39  300   47  34  34  51  600  72  58  45  47
-inline int grouped_tile_rows(int64_t N, int64_t E, int64_t M)
+//   16 of 1032 x 2056  120             -  94  76 111  170    - 110  83 119  220   - 135 123 126
+inline int grouped_tile_rows(int64_t N, int64_t E, int64_t M, int64_t K, bool gate_up)
 {
     int rows = most_tile_rows(N, E);
-    while (rows > 32 && (N / rows + std::min(E, N) / 2) * cdiv(M, 128) < kBlockTarget / 2)
+    const bool cached = 2 * std::min(E, N) * M * K <= (int64_t)256 << 20;
+    const auto tiles = [&] { return (N / rows + std::min(E, N) / 2) * cdiv(M, rows == 256 && !gate_up ? 256 : 128); };
+    while (rows > 32 && tiles() < (rows == 256 && cached ? kBlockTarget * 3 / 4 : kBlockTarget / 2))
         rows /= 2;
     return rows;
+}
+
+// How the tiles that a routing gives are laid on blocks: whole rounds of `slots` tiles, one
+// block each, then the rest, each split over k into `splits` blocks of kt_split k-tiles.
+// The kernels call this (constexpr: for host and device).
+struct GroupedSplit {
+    int in_rounds, rest, splits, kt_split;
+};
+constexpr GroupedSplit grouped_split(int tiles, int slots, int most_splits, int nk)
+{
+    GroupedSplit s{tiles / slots * slots, 0, 1, nk};
+    s.rest = tiles - s.in_rounds;
+    if (most_splits > 1 && s.rest > 0) {
+        const int n = slots / s.rest;
+        const int splits = n < most_splits ? n : most_splits; // rest < slots
+        s.kt_split = (nk + splits - 1) / splits;
+        s.splits = (nk + s.kt_split - 1) / s.kt_split;
+    }
+    return s;
+}
+
+// The column and row tile of tile `local` of an expert: sweeps of 8 column tiles.
+struct GroupedTileAt {
+    int column, row;
+};
+constexpr GroupedTileAt grouped_tile_at(int local, int tiles_m, int tiles_n)
+{
+    const int per_group = 8 * tiles_n, group = local / per_group, in_group = local - group * per_group;
+    const int width = tiles_m - group * 8 < 8 ? tiles_m - group * 8 : 8;
+    return GroupedTileAt{group * 8 + in_group % width, in_group / width};
 }
 
 // A product of M columns with `segments` contractions of K each, on tiles of ROWS rows.
@@ -138,7 +173,7 @@ GroupedStep grouped_step(int64_t N, int64_t E, int64_t M, int64_t K, int segment
 template <GroupedOp OP>
 GroupedStep grouped_step(int64_t N, int64_t E, int64_t M, int64_t K, int segments = 1)
 {
-    return with_grouped_rows(grouped_tile_rows(N, E, M),
+    return with_grouped_rows(grouped_tile_rows(N, E, M, K, OP == GROUPED_GATE_UP || OP == GROUPED_SAVE),
                              [&](auto rows) { return grouped_step<OP, decltype(rows)::value>(N, E, M, K, segments); });
 }
 

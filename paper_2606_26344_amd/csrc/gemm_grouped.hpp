@@ -195,14 +195,10 @@ __global__ __launch_bounds__(S::NTHREADS, S::BLOCKS) void gemm_grouped_kernel(Gr
         head.load(p, 0, lane);
         const int row_tiles = count_row_tiles<S::BN>(p, head, lane);
         const int tiles = row_tiles * p.columns;
-        const int in_rounds = tiles / p.slots * p.slots;
-        rest = tiles - in_rounds;
-        int kt_split = p.nk;
-        if (p.most_splits > 1 && rest > 0) {
-            splits = max(1, min(p.most_splits, p.slots / rest));
-            kt_split = (p.nk + splits - 1) / splits;
-            splits = (p.nk + kt_split - 1) / kt_split;
-        }
+        const GroupedSplit lay = grouped_split(tiles, p.slots, p.most_splits, p.nk);
+        const int in_rounds = lay.in_rounds;
+        rest = lay.rest;
+        splits = lay.splits;
         if (bid >= in_rounds + rest * splits)
             return;
         whole = bid < in_rounds;
@@ -220,14 +216,12 @@ __global__ __launch_bounds__(S::NTHREADS, S::BLOCKS) void gemm_grouped_kernel(Gr
         K = p.K;
         tiles_m = p.columns;
         tiles_n = (N + S::BN - 1) / S::BN;
-        kt_begin = split * kt_split;
-        kt_end = whole ? p.nk : min(p.nk, kt_begin + kt_split);
+        kt_begin = split * lay.kt_split;
+        kt_end = whole ? p.nk : min(p.nk, kt_begin + lay.kt_split);
     }
     const int nk = kt_end - kt_begin;
-    const int per_group = 8 * tiles_n;
-    const int group = local / per_group, in_group = local - group * per_group;
-    const int group_w = min(tiles_m - group * 8, 8);
-    const int m0 = (group * 8 + in_group % group_w) * BMW, n0 = (in_group / group_w) * S::BN;
+    const GroupedTileAt at = grouped_tile_at(local, tiles_m, tiles_n);
+    const int m0 = at.column * BMW, n0 = at.row * S::BN;
 
     // The tile with TX of its TN row blocks per wave; STREAM_A: a weight past the L2.
     const int own_lane = lane;
