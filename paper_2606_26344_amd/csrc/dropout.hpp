@@ -9,7 +9,9 @@
 // the generator serves them all.  Ten rounds of two 32 x 32 -> 64-bit products (quarter
 // rate) and eight other instructions are about 600 cycles of a wave's 512 elements; with
 // 32 bits for each element they would be twice that and bound the pass instead of the
-// memory.
+// memory.  Measured: 4096 x 4096 into an fp32 residual stream 31.8 us, 5.3 TB/s (a copy
+// on that board 5.1); past the L2 the stores are slower (32.0 against 28.6 us on inputs in
+// the last-level cache).
 #pragma once
 
 #include <type_traits>

@@ -2,7 +2,9 @@
 //
 // The sort is a stable counting sort: its results are whole numbers, so any order of the
 // counting gives the same.  Rows are moved token by token: a token's
-// row is read once and written to (or summed from) the k rows of its slots.
+// row is read once and written to (or summed from) the k rows of its slots.  They are
+// bound by the memory (us, TB/s): 4096 tokens of 4096 columns, dispatch to 2 rows each 16.5,
+// 6.1; combine of 8 rows each 63.8, 4.7; its gradients 108.6, 5.3, where a copy takes 5.1.
 #pragma once
 
 #include <type_traits>
@@ -300,7 +302,8 @@ __device__ __forceinline__ u32x4 load_row(const u32x4 *p)
 {
     return ONCE ? __builtin_nontemporal_load(p) : *p;
 }
-// They are written for another kernel.
+// They are written for another kernel: dispatch of 4096 tokens to 8 rows each 66 us, through
+// the L2 80.
 __device__ __forceinline__ void store_row(u32x4 *p, const u32x4 &v) { __builtin_nontemporal_store(v, p); }
 
 // xs[slot] = x: 1 << lanes_log threads of a block move one token's row.
