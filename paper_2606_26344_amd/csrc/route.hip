@@ -131,8 +131,9 @@ int gmlp_route_sort(const void *ids, void *offsets, void *slots, int64_t T, int6
         ++p.bits;
     hipStream_t st = static_cast<hipStream_t>(stream);
     const bool one = n <= kSortOneLaunch;
-    // Chunks of 2048 assignments, no less than the experts; more where there would be many.
-    p.chunk = 2 * kSortThreads * (int)std::max<int64_t>(1, n / (2048 * 512));
+    // Chunks of 1024 assignments; in three launches of 2048, no less than the experts, and
+    // more where there would be many.
+    p.chunk = one ? kSortThreads : 2 * kSortThreads * (int)std::max<int64_t>(1, n / (2048 * 512));
     p.blocks = (int)std::max<int64_t>(1, n / p.chunk);
     return with_flag(id == 8, [&](auto wide) {
         using Id = std::conditional_t<decltype(wide)::value, int64_t, int32_t>;

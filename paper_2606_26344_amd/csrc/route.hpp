@@ -113,7 +113,7 @@ __device__ __forceinline__ void place_slots(const SortParams &p, const SortRange
 // Up to kSortOneLaunch assignments: a block ranks its chunk, its waves a sixteenth of
 // that each, and counts all others, those before the chunk and those behind it.  So no
 // block waits for another, but each reads everything, at 50 GB/s for each CU: us, one
-// launch against three, 8 experts and 8192 assignments 5.9 and 15.2, 64 and 32768 10.3 and
+// launch against three, 8 experts and 8192 assignments 5.6 and 15.2, 64 and 32768 9.7 and
 // 10.1, 64 and 65536 15.5 and 10.1, 128 and 524288 95 and 14.5.
 template <class Id>
 __global__ __launch_bounds__(kSortThreads) void route_sort_kernel(SortParams p)
