@@ -84,6 +84,19 @@ auto with_grouped_rows(int rows, F f)
 // Rows of an expert where they are spread evenly over as many experts as can have some.
 inline double rows_per_expert(int64_t N, int64_t E) { return (double)N / (double)std::max<int64_t>(1, std::min(N, E)); }
 
+// The most splits of a tile of nk k-tiles: tiles that do not fill the chip are split over k,
+// into the count with the least of the k-tiles' time and that of the exchange, n x (as in
+// split_time), if that gains.
+template <class S>
+int grouped_splits(int nk)
+{
+    const double bytes = (double)S::BM * S::BN * sizeof(float);
+    const double x = bytes / 54e3 + bytes * kBlockTarget * S::BLOCKS / 8e6 / 4;
+    const double whole = nk * grad_tile_time<S>();
+    const int n = (int)std::min(std::sqrt(whole / x), (double)std::max(1, nk / 2));
+    return n >= 2 && whole - whole / n > 4.0 + n * x ? n : 1;
+}
+
 // The most rows that a tile of a call has: where the weights fill the chip with tiles, those
 // that the experts' rows go into once, with room for more than the mean.
 inline int most_tile_rows(int64_t N, int64_t E)
@@ -93,8 +106,9 @@ inline int most_tile_rows(int64_t N, int64_t E)
 }
 
 // Rows of a tile of a product with M columns and K contracted elements: fewer, down to 32,
-// while half the CUs have no tile.  Weights that the last-level cache holds may be read
-// by two tiles of 128 rows for one of 256: there a quarter of the CUs without will do.
+// while half the CUs have no tile, or, of kManySplits k-tiles and more, split of one.
+// Weights that the last-level cache holds may be read by two tiles of 128 rows for one of
+// 256: there a quarter of the CUs without will do.
 // Measured with each (forward pass, us, for 32, 64, 128 and 256 rows; rows of experts
 // spread by 3 : 1):
 //   8 of 4096 x 14336   16 rows each 455 455 467 530   32  594 469 477 540   64 1042 729 509 561
@@ -102,13 +116,25 @@ inline int most_tile_rows(int64_t N, int64_t E)
 //   32 of 2048 x 1024   32            92  74  76  82   64  147 106  83  84  128 232 155 130 101
 //   8 of 1024 x 512     64            23  27  30  39  300   47  34  34  51  600  72  58  45  47
 //   16 of 1032 x 2056  120             -  94  76 111  170    - 110  83 119  220   - 135 123 126
-inline int grouped_tile_rows(int64_t N, int64_t E, int64_t M, int64_t K, bool gate_up)
+// Splits for tiles, and tiles only: one expert of 4096 x 14336, 60 rows 80 and 102, 150 rows 113
+// and 187; four of 2048 x 1024 (16 and 32 k-tiles), 150 rows 36 and 30.
+constexpr int kManySplits = 64;
+template <GroupedOp OP>
+int grouped_tile_rows(int64_t N, int64_t E, int64_t M, int64_t K, int segments)
 {
     int rows = most_tile_rows(N, E);
-    const bool cached = 2 * std::min(E, N) * M * K <= (int64_t)256 << 20;
-    const auto tiles = [&] { return (N / rows + std::min(E, N) / 2) * cdiv(M, rows == 256 && !gate_up ? 256 : 128); };
-    while (rows > 32 && tiles() < (rows == 256 && cached ? kBlockTarget * 3 / 4 : kBlockTarget / 2))
-        rows /= 2;
+    const int64_t experts = std::min(E, N); // with rows, at most
+    const bool cached = 2 * experts * M * K <= (int64_t)256 << 20;
+    for (; rows > 32; rows /= 2) {
+        const int64_t blocks = with_grouped_rows(rows, [&](auto r) {
+            using S = GroupedTile<OP, decltype(r)::value>;
+            const int64_t tiles = std::max(experts, N / rows + experts / 2) * cdiv(M, grouped_columns<OP, S>());
+            const int nk = segments * (int)cdiv(K, S::BK);
+            return rows == 256 || nk < kManySplits ? tiles : tiles * grouped_splits<S>(nk);
+        });
+        if (blocks >= (rows == 256 && cached ? kBlockTarget * 3 / 4 : kBlockTarget / 2))
+            break;
+    }
     return rows;
 }
 
@@ -155,13 +181,7 @@ GroupedStep grouped_step(int64_t N, int64_t E, int64_t M, int64_t K, int segment
     // Every expert with rows has one tile that may not be full.
     s.most_row_tiles = (int)std::min<int64_t>(N / ROWS + std::min(E, N), N);
     s.slots = kBlockTarget * S::BLOCKS;
-    // Tiles that do not fill the chip are split over k: the count with the least of the
-    // k-tiles' time and that of the exchange, n x (as in split_time), if that gains.
-    const double per = grad_tile_time<S>(), bytes = (double)S::BM * S::BN * sizeof(float);
-    const double x = bytes / 54e3 + bytes * s.slots / 8e6 / 4;
-    const double whole = s.nk * per;
-    const int n = (int)std::min(std::sqrt(whole / x), (double)std::max(1, s.nk / 2));
-    s.most_splits = n >= 2 && whole - whole / n > 4.0 + n * x ? n : 1;
+    s.most_splits = grouped_splits<S>(s.nk);
     s.blocks = (int64_t)s.most_row_tiles * s.columns;
     if (s.most_splits > 1)
         s.blocks = s.blocks / s.slots * s.slots + s.slots;
@@ -173,7 +193,7 @@ GroupedStep grouped_step(int64_t N, int64_t E, int64_t M, int64_t K, int segment
 template <GroupedOp OP>
 GroupedStep grouped_step(int64_t N, int64_t E, int64_t M, int64_t K, int segments = 1)
 {
-    return with_grouped_rows(grouped_tile_rows(N, E, M, K, OP == GROUPED_GATE_UP || OP == GROUPED_SAVE),
+    return with_grouped_rows(grouped_tile_rows<OP>(N, E, M, K, segments),
                              [&](auto rows) { return grouped_step<OP, decltype(rows)::value>(N, E, M, K, segments); });
 }
 
