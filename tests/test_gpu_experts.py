@@ -7,10 +7,16 @@ sum of products of bf16 numbers, rounded once to bf16 (2^-8 of the value).  Befo
     of the terms' absolute values;
   * H, dG and dU are rounded to bf16: 2^-8 of the terms of the sums that they enter, and
     act and act' in fp32 (exp and rcp to 2 units in the last place) 2^-20;
-  * dH in fp32 carries 2^-12 of its terms into dG and dU.
+  * dH in fp32 carries 2^-12 of its terms into dG and dU; dX sums 2 F <= 8208 products,
+    formed 32 at a time: 257 roundings of 2^-24 S, and the weights' gradients fewer.
 
 So results are within 2^-8 |ref| + 1.02 2^-8 S + 2^-12 S, and G and U within 2^-8 |ref| +
-2^-12 S.
+2^-12 S.  S is some sqrt(K) times the result where K products add up, and a block of k that
+is left out would hide in it; so each expert's results are compared as a whole too.  A
+rounding moves a tensor by at most 2^-8 of its L2 norm, and a product with a random
+matrix has about the same gain for that as for the tensor: with the roundings of the
+operands (H; dG and dU) and of the result 3 2^-8 of its norm.  64 of 4104 terms left out
+would be 2^-3.
 """
 import pytest
 import torch
@@ -52,6 +58,8 @@ def check(name, got, ref, terms, rounded=True):
     bound = HALF_STEP * ref.abs() + (ROUNDED if rounded else 2.0 ** -12) * terms + 1e-30
     ratio = ((got.double() - ref).abs() / bound).max().item() if ref.numel() else 0.0
     assert ratio <= 1.0, (name, ratio)
+    off = (got.double() - ref).norm().item()
+    assert off <= 3 * HALF_STEP * ref.norm().item(), (name, off)
     return ratio
 
 
@@ -132,6 +140,32 @@ TILES = [([20, 24, 1, 30, 7], 1032, 2056), ([2, 0, 0, 0, 0, 0, 0, 0], 2056, 4104
 @pytest.mark.parametrize("counts,D,F", TILES, ids=[str(i) for i in range(len(TILES))])
 def test_tiles(counts, D, F):
     run(counts, D, F, 3, seed=D + len(counts))
+
+
+# The 256-row tiles, with last tiles of up to 64, 128 and 256 rows of experts with one tile and
+# with several; the others with splits of long products; weight gradients in whole lines.
+RAGGED = [300, 511, 1, 700, 260, 64, 129, 400, 0, 100, 356]
+MORE_TILES = [(RAGGED, 4096, 4096), (RAGGED, 4104, 4104), ([30, 33, 20, 40, 1, 29], 2056, 4104), ([40, 30], 4104, 4104),
+              ([90, 120, 70], 4104, 4104), ([110, 60, 100, 90], 1024, 4096), ([1700, 1600], 256, 512), ([9, 2, 0, 4], 4096, 1024),
+              ([150, 200], 512, 4096)]
+
+
+@pytest.mark.parametrize("counts,D,F", MORE_TILES, ids=[str(i) for i in range(len(MORE_TILES))])
+def test_more_tiles(counts, D, F):
+    run(counts, D, F, 3, seed=D + F + len(counts))
+
+
+def test_every_tile_is_tested():
+    names, split = set(), set()
+    for counts, D, F in [(c[0], c[1], c[2]) for c in SMALL] + TILES + MORE_TILES:
+        for backward in (False, True):
+            for name, _, _, splits in experts.describe(sum(counts) + 3, len(counts), D, F, backward):
+                names.add(name)
+                if splits > 1:
+                    split.add(name)
+    # Gate/up, down, dH and dX on four tiles each, the weight gradients on three and both ways out.
+    assert len(names) == 4 * 4 + 3 * 2
+    assert len(split) == 4 * 4
 
 
 @pytest.mark.parametrize("activation,beta", [("swish", 1.702), ("sigmoid", 1.0), ("swish", -0.5)])
