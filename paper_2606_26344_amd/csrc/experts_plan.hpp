@@ -97,12 +97,27 @@ int grouped_splits(int nk)
     return n >= 2 && whole - whole / n > 4.0 + n * x ? n : 1;
 }
 
-// The most rows that a tile of a call has: where the weights fill the chip with tiles, those
-// that the experts' rows go into once, with room for more than the mean.
+// The most rows that a tile of a call has.
 inline int most_tile_rows(int64_t N, int64_t E)
 {
     const double n = rows_per_expert(N, E);
-    return n <= 20 ? 32 : n <= 40 ? 64 : n <= 112 ? 128 : 256;
+    return n <= 20 ? 32 : n <= 40 ? 64 : n <= 100 ? 128 : 256;
+}
+
+// Time (us) of tiles of ROWS rows for experts with fewer of them each: whole rounds, and a
+// last one whose tiles are split.  A tile of 256 rows leaves out its upper half.
+template <GroupedOp OP, int ROWS>
+double grouped_rounds_time(int64_t N, int64_t E, int64_t M, int64_t K, int segments)
+{
+    using S = GroupedTile<OP, ROWS>;
+    const int nk = segments * (int)cdiv(K, S::BK);
+    const int64_t experts = std::min(E, N), tiles = std::max(experts, N / ROWS + experts / 2) * cdiv(M, grouped_columns<OP, S>());
+    const int64_t slots = kBlockTarget * S::BLOCKS, rest = tiles % slots;
+    double rounds = std::max<double>(1.0, (double)(tiles / slots));
+    if (tiles > slots && rest)
+        rounds += 2 * rest > slots ? 1.0 : 0.1 + 1.0 / (double)std::min<int64_t>(grouped_splits<S>(nk), slots / rest);
+    const double per = ROWS == 256 ? (S::A_BYTES + 128 * S::BK * 2) / 50e3 : grad_tile_time<S>();
+    return rounds * (nk * per + 8.0);
 }
 
 // Rows of a tile of a product with M columns and K contracted elements: fewer, down to 32,
@@ -122,7 +137,16 @@ constexpr int kManySplits = 64;
 template <GroupedOp OP>
 int grouped_tile_rows(int64_t N, int64_t E, int64_t M, int64_t K, int segments)
 {
-    int rows = most_tile_rows(N, E);
+    // Where the weights fill the chip with tiles, those that the experts' rows go into once,
+    // with room for more than the mean; and, since experts with more rows than 128 take two
+    // tiles, above 100 rows those of 256 where they save a round (us, forward, 110 rows each:
+    // 32 experts of 2048 x 1024 117 and 97, 64 213 and 192; at 68 to 95 rows they lose as
+    // often as they gain).
+    const double n = rows_per_expert(N, E);
+    int rows = n <= 20 ? 32 : n <= 40 ? 64 : n <= 112 ? 128 : 256;
+    if (rows == 128 && n > 100 &&
+        grouped_rounds_time<OP, 256>(N, E, M, K, segments) < 0.9 * grouped_rounds_time<OP, 128>(N, E, M, K, segments))
+        rows = 256;
     const int64_t experts = std::min(E, N); // with rows, at most
     const bool cached = 2 * experts * M * K <= (int64_t)256 << 20;
     for (; rows > 32; rows /= 2) {
