@@ -13,10 +13,9 @@
  * before offsets[0]) are neither read nor written in any tensor.
  *
  * The offsets are in device memory: how many rows an expert has is known to the kernels
- * only, and no call waits for it.  They are taken within 0 .. N, and an expert whose end
- * is before its begin has no rows; experts whose rows overlap, which no sort gives, leave
- * undefined values in rows of Y (and G, U, dX), or of as many as N / 32 + E tiles of rows
- * hold, and nowhere else.
+ * only, and no call waits for it.  They are taken within 0 .. N and as never falling: an
+ * offset below one before it, which no sort gives, counts as that one, so that no row is
+ * two experts' and one whose end is not past its begin has none.
  *
  * Numerics, activations and beta as in gmlp.h and gmlp_train.h: bfloat16 tensors, fp32
  * accumulation, H (and dG, dU) rounded once to bf16 where they are operands, results

@@ -40,6 +40,7 @@ GroupedParams grouped_params(const void *offsets, int64_t N, int64_t E, uint8_t 
 {
     GroupedParams p{};
     p.offsets = static_cast<const int32_t *>(offsets);
+    p.offsets_fall = reinterpret_cast<int32_t *>(ws + l.fall_off);
     p.experts = (int)E;
     p.rows = (int)N;
     p.partial = reinterpret_cast<float *>(ws + l.partial_off);

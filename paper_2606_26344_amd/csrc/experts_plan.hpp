@@ -162,6 +162,19 @@ int grouped_tile_rows(int64_t N, int64_t E, int64_t M, int64_t K, int segments)
     return rows;
 }
 
+// The rows of an expert within 0 .. rows, whatever the offsets hold: `from` is the largest of the
+// offsets up to its own, which sorted offsets are themselves, `to` the one behind it.  So no
+// row is two experts', and N rows have at most the tiles that a grid is for.  The kernels
+// call this.
+struct GroupedRows {
+    int first, count;
+};
+constexpr GroupedRows grouped_rows(int from, int to, int rows)
+{
+    const int first = std::min(std::max(from, 0), rows);
+    return GroupedRows{first, std::min(std::max(to, first), rows) - first};
+}
+
 // How the tiles that a routing gives are laid on blocks: whole rounds of `slots` tiles, one
 // block each, then the rest, each split over k into `splits` blocks of kt_split k-tiles.
 // The kernels call this (constexpr: for host and device).
@@ -279,9 +292,10 @@ inline GroupedPlan grouped_plan(int64_t N, int64_t E, int64_t D, int64_t F)
     return p;
 }
 
-// The workspace: counters, H, dG and dU, the partial sums of one step.
+// The workspace: counters, a word of the backward pass, H, dG and dU, the partial sums of one
+// step.
 struct GroupedLayout {
-    size_t h_off = 0, dg_off = 0, du_off = 0, partial_off = 0, total = 0;
+    size_t fall_off = 0, h_off = 0, dg_off = 0, du_off = 0, partial_off = 0, total = 0;
     int counters = 0;
 };
 
@@ -289,7 +303,8 @@ inline GroupedLayout grouped_layout(int64_t N, int64_t E, int64_t D, int64_t F)
 {
     GroupedLayout l;
     const size_t h = align_up((size_t)N * F * 2);
-    l.h_off = kCounterBytes;
+    l.fall_off = kCounterBytes;
+    l.h_off = l.fall_off + kAlign;
     l.dg_off = l.h_off + h;
     l.du_off = l.dg_off + h;
     l.partial_off = l.du_off + h;

@@ -11,9 +11,9 @@ Argument marshalling only.  Names mirror the C entry points:
 
 xs, ys, dxs, dys [N, D] and g, u [N, F] are ``torch.bfloat16``, as are the weights wg, wu
 [E, D, F] and wd [E, F, D]; offsets [E + 1] is int32: expert e has the rows offsets[e] ..
-offsets[e + 1] - 1.  Rows that no expert has are not written.  All contiguous, on one HIP
-device.  Without a workspace the calls take memory for one call from torch's caching
-allocator.
+offsets[e + 1] - 1 (offsets that fall count as their running maximum).  Rows that no expert
+has are not written.  All contiguous, on one HIP device.  Without a workspace the calls
+take memory for one call from torch's caching allocator.
 """
 from __future__ import annotations
 
