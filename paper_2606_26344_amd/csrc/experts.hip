@@ -53,6 +53,15 @@ GroupedParams grouped_params(const void *offsets, int64_t N, int64_t E, uint8_t 
 const uint16_t *bf16(const void *p) { return static_cast<const uint16_t *>(p); }
 uint16_t *bf16(void *p) { return static_cast<uint16_t *>(p); }
 
+int launch_grouped(void (*kernel)(GroupedParams), const GroupedStep &s, GroupedParams p, const char *what, hipStream_t st)
+{
+    return with_launches(s, [&](int64_t first, int64_t blocks) {
+        p.first_block = (int)first;
+        hipLaunchKernelGGL(kernel, dim3((unsigned)blocks), dim3((unsigned)s.threads), 0, st, p);
+        return hip_check(hipGetLastError(), what);
+    });
+}
+
 // A product with a weight, of M columns and segments of K.
 template <GroupedOp OP>
 int launch_rows(const GroupedStep &s, const GroupedLayout &l, GroupedParams p, int64_t M, int64_t K, const char *what, hipStream_t st)
@@ -69,8 +78,7 @@ int launch_rows(const GroupedStep &s, const GroupedLayout &l, GroupedParams p, i
     p.most_splits = s.most_splits;
     return with_grouped_rows(s.rows, [&](auto rows) {
         using S = GroupedTile<OP, decltype(rows)::value>;
-        hipLaunchKernelGGL((gemm_grouped_kernel<S, OP, false>), dim3((unsigned)s.blocks), dim3(S::NTHREADS), 0, st, p);
-        return hip_check(hipGetLastError(), what);
+        return launch_grouped(gemm_grouped_kernel<S, OP, false>, s, p, what, st);
     });
 }
 
@@ -90,26 +98,30 @@ int launch_weights(const GroupedStep &s, GroupedParams p, hipStream_t st)
     return with_grouped_weight_tile((GradTile)s.rows, [&](auto tag) {
         using S = typename decltype(tag)::type;
         auto *kernel = stream_weight_outputs(p) ? gemm_grouped_kernel<S, GROUPED_DW, true> : gemm_grouped_kernel<S, GROUPED_DW, false>;
-        hipLaunchKernelGGL(kernel, dim3((unsigned)s.blocks), dim3(S::NTHREADS), 0, st, p);
-        return hip_check(hipGetLastError(), "weight gradient launch");
+        return launch_grouped(kernel, s, p, "weight gradient launch", st);
     });
 }
 
 template <class S>
-std::string grouped_line(const GroupedStep &s, int op, bool stream)
+std::string grouped_lines(const GroupedStep &s, int op, bool stream)
 {
-    char tmp[200];
-    snprintf(tmp, sizeof tmp,
-             "gemm_grouped_kernel<GradShape<%d, %d, %d, %d, %d, %d, %d>, (GroupedOp)%d, %s> grid=%lld block=%d k_splits=%d\n", S::WM,
-             S::WN, S::TM, S::TN, S::STAGES, S::BK, S::BLOCKS, op, stream ? "true" : "false", (long long)s.blocks, s.threads,
-             s.most_splits);
-    return tmp;
+    std::string text;
+    with_launches(s, [&](int64_t, int64_t blocks) {
+        char tmp[200];
+        snprintf(tmp, sizeof tmp,
+                 "gemm_grouped_kernel<GradShape<%d, %d, %d, %d, %d, %d, %d>, (GroupedOp)%d, %s> grid=%lld block=%d k_splits=%d\n",
+                 S::WM, S::WN, S::TM, S::TN, S::STAGES, S::BK, S::BLOCKS, op, stream ? "true" : "false", (long long)blocks,
+                 s.threads, s.most_splits);
+        text += tmp;
+        return 0;
+    });
+    return text;
 }
 
 template <GroupedOp OP>
-std::string rows_line(const GroupedStep &s)
+std::string rows_lines(const GroupedStep &s)
 {
-    return with_grouped_rows(s.rows, [&](auto rows) { return grouped_line<GroupedTile<OP, decltype(rows)::value>>(s, OP, false); });
+    return with_grouped_rows(s.rows, [&](auto rows) { return grouped_lines<GroupedTile<OP, decltype(rows)::value>>(s, OP, false); });
 }
 
 } // namespace
@@ -133,13 +145,13 @@ int gmlp_experts_describe(int64_t N, int64_t E, int64_t D, int64_t F, int backwa
     std::string text;
     if (!backward) {
         if (N > 0)
-            text = rows_line<GROUPED_GATE_UP>(p.gate_up) + rows_line<GROUPED_DOWN>(p.down);
+            text = rows_lines<GROUPED_GATE_UP>(p.gate_up) + rows_lines<GROUPED_DOWN>(p.down);
     } else {
         if (N > 0)
-            text = rows_line<GROUPED_DH>(p.dh) + rows_line<GROUPED_DX>(p.dx);
+            text = rows_lines<GROUPED_DH>(p.dh) + rows_lines<GROUPED_DX>(p.dx);
         // The outputs taken as starting on 128-byte lines.
         text += with_grouped_weight_tile((GradTile)p.dw.rows, [&](auto tag) {
-            return grouped_line<typename decltype(tag)::type>(p.dw, GROUPED_DW, D % 64 == 0 && F % 64 == 0);
+            return grouped_lines<typename decltype(tag)::type>(p.dw, GROUPED_DW, D % 64 == 0 && F % 64 == 0);
         });
     }
     snprintf(buf, bytes, "%s", text.c_str());

@@ -68,6 +68,24 @@ struct GroupedStep {
     size_t partial_bytes = 0;
 };
 
+// A launch has fewer than 2^32 threads, and the blocks of a step are launched in parts of at
+// most this: more than one for the gradients of hundreds of wide and narrow weights (1024 of
+// 8 x 2^20: 25 million tiles).  A multiple of 8, so that a block's number in its launch and
+// among all give the same XCD.
+constexpr int64_t grouped_launch_blocks(int threads) { return ((int64_t(1) << 32) - 1) / threads / 8 * 8; }
+
+// f(blocks before, blocks) of each part.
+template <class F>
+int with_launches(const GroupedStep &s, F f)
+{
+    for (int64_t first = 0; first < s.blocks; first += grouped_launch_blocks(s.threads)) {
+        const int rc = f(first, std::min(s.blocks - first, grouped_launch_blocks(s.threads)));
+        if (rc)
+            return rc;
+    }
+    return GMLP_OK;
+}
+
 // f(integral_constant<rows>) of a tile.
 template <class F>
 auto with_grouped_rows(int rows, F f)
@@ -335,10 +353,6 @@ inline int check_experts_shape(int64_t N, int64_t E, int64_t D, int64_t F)
         return fail(GMLP_ERR_UNSUPPORTED, "shape N=%lld E=%lld D=%lld F=%lld exceeds the supported range (E <= %d, D, F <= %d, "
                     "N <= %lld, at most %lld elements per tensor)", (long long)N, (long long)E, (long long)D, (long long)F,
                     GMLP_MAX_EXPERTS, GMLP_EXPERTS_MAX_WIDTH, (long long)kMaxTokens, (long long)kMaxElements);
-    const GroupedPlan p = grouped_plan(N, E, D, F);
-    for (const GroupedStep *s : {&p.gate_up, &p.down, &p.dh, &p.dx, &p.dw})
-        if (s->blocks * s->threads >= (int64_t(1) << 32) || s->blocks >= (int64_t(1) << 31))
-            return fail(GMLP_ERR_UNSUPPORTED, "%lld blocks exceed a launch grid", (long long)s->blocks);
     return GMLP_OK;
 }
 

@@ -44,6 +44,7 @@ struct GroupedParams {
     int columns, most_row_tiles, slots, most_splits;
     int pM[3], pN[3]; // weight gradients: columns and rows of each
     int problems, problem_tiles;
+    int first_block; // of this launch
     float *partial;
     uint32_t *counters;
     const uint16_t *g, *u; // GROUPED_DH
@@ -195,7 +196,7 @@ __global__ __launch_bounds__(S::NTHREADS, S::BLOCKS) void gemm_grouped_kernel(Gr
     const int tid = threadIdx.x, lane = tid & 63;
     const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int wm = wave % S::WM, wn = wave / S::WM;
-    const int bid = blockIdx.x;
+    const int bid = p.first_block + (int)blockIdx.x;
 
     // ---- block -> tile ---------------------------------------------------------
     // As in gemm_grad.hpp: each XCD takes a contiguous range of the tiles, an expert's
