@@ -159,7 +159,11 @@ int grouped_tile_rows(int64_t N, int64_t E, int64_t M, int64_t K, int segments)
     // with room for more than the mean; and, since experts with more rows than 128 take two
     // tiles, above 100 rows those of 256 where they save a round (us, forward, 110 rows each:
     // 32 experts of 2048 x 1024 117 and 97, 64 213 and 192; at 68 to 95 rows they lose as
-    // often as they gain).
+    // often as they gain).  From 113 on 256 whatever the rounds, which is not always the
+    // faster (us, forward, this rule and 128 rows, at 115, 130, 170 and 200 rows each: 64
+    // experts of 2048 x 1408 266 283, 271 302, 298 341, 344 378; 8 of 4096 x 14336 640 759, 654
+    // 683, 665 791, 896 875; 32 of 2048 x 1024 100 119, 101 125, 150 135, 162 141; 16 of 1032 x
+    // 2056, whose down step has 128 either way, 96 87, 100 84, 101 80, 106 95).
     const double n = rows_per_expert(N, E);
     int rows = n <= 20 ? 32 : n <= 40 ? 64 : n <= 112 ? 128 : 256;
     if (rows == 128 && n > 100 &&

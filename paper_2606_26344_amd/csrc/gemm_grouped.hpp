@@ -21,8 +21,8 @@
 // Few rows are bound by the weights: 2 of 8 experts of 4096 x 14336 with a row each 80 us
 // gate/up and 40 down, 5.9 TB/s.  Many by the matrix cores, as the kernels for one MLP: 8192
 // rows of one expert 1608 us gate/up, 700 down, 963 dH, 1406 dX, 2322 the weight gradients,
-// 1.19, 1.37, 1.00, 1.37 and 1.24 PFLOP/s; of 8 experts with 558 to 1879 rows 1854, 851, 1094,
-// 1717 and 2759, for the tiles of few rows at the experts' ends (half a whole one's time)
+// 1.19, 1.37, 1.00, 1.37 and 1.24 PFLOP/s; of 8 experts with 558 to 1879 rows 1821, 838, 1092,
+// 1715 and 2718, for the tiles of few rows at the experts' ends (half a whole one's time)
 // and a last round that is not full.
 #pragma once
 
